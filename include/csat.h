@@ -239,6 +239,84 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
                                 void* C, void* Z, float* X, void* stream);
 
 /* ------------------------------------------------------------------------------------------------------
+ * Exact attention next to the compressed block, and the cache that serves it: softmax(scale Q K^T) V over packed
+ * sequences (what the compressed block approximates; the layers of a hybrid model that keep it), the keys and
+ * values of past tokens in 8 bits, attention of new tokens over them, and the removal of the least attended.
+ *
+ * Packed rows: the rows of all sequences one behind the other; sequence b's rows of Q and O are q_offsets[b] ..
+ * q_offsets[b+1], those of K and V k_offsets[b] .. k_offsets[b+1] (device int32 [B+1], not decreasing, within
+ * n_q / n_k; sequences may be empty).  Row r, head h starts at element r * token stride + h * head stride of its
+ * tensor; strides are multiples of 16 bytes (so a part of a fused projection serves as well as a tensor of its own, and 0
+ * repeats a row), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
+ * max_q, max_k bound the rows of one sequence: rows beyond the bound are not computed and not written.  So are rows
+ * of no sequence (behind the last offset): they are left as they were.
+ * d: a multiple of 8 (csat_prompt_attention) or of 16 (the cache), at most 256.  n_q, n_k, max_q, max_k at least 1.
+ * ------------------------------------------------------------------------------------------------------ */
+typedef struct {
+    int B, Hq, Hkv, d;
+    int n_q, n_k, max_q, max_k;
+    int causal;               /* row i of n rows sees the first n_keys - n + i + 1 keys (aligned at the end); 0: all keys */
+    csat_dtype dtype;         /* Q, K, V and O; lse, weights and every accumulation are float */
+    long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   /* strides, elements */
+} csat_packed_dims;
+
+/* O = softmax(scale Q K^T) V per sequence and head, by one pass over the keys with a running maximum and sum.
+ * scale > 0.  lse (float [Hq, n_q], optional): the logarithm of each row's sum of exp(scale q.k).  A row that sees no key
+ * (an empty sequence, causal with fewer keys than rows), or only scores of -inf, is 0 with lse = -inf.  What a masked
+ * or foreign row of K or V holds, an infinity or NaN included, has no effect.  bf16: the weights are rounded to bf16 (by at
+ * most 2^-8 of each) for the product with V, everything else is float.
+ * Workspace: csat_prompt_workspace_bytes (host-only query; it may be 0, workspace may then be NULL). */
+csat_status csat_prompt_workspace_bytes(const csat_packed_dims* dims, size_t* bytes);
+csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const void* Q, const void* K, const void* V,
+                                  const int* q_offsets, const int* k_offsets, float scale, void* O, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Key/value cache in 8 bits.  The pool holds `pages` pages; a block is one page of one head: `page` tokens (16, 32, 64
+ * or 128) of e4m3 codes that share one scale, a power of two (Ks, Vs, float [pages, Hkv]); a value is code * scale.  K codes lie
+ * [pages, Hkv, page, d], V codes [pages, Hkv, d, page] (a token's values a page apart, the order in which the
+ * attention's matrix instructions take them).  A sequence's tokens are the first lengths[b] slots of the pages that row b of
+ * table (device int32 [B, max_pages]) names; entries beyond them are not read.  max_len bounds lengths[b] (it sizes
+ * the grids; at most max_pages * page).  Pages may be shared by sequences as long as they are only read.
+ * Errors in what only the device sees: a sequence whose length is negative or above max_len, or one of whose needed
+ * table entries names no page of the pool, gives NaN in its rows of O and lse (its weights are then undefined), is not
+ * stored to, and is evicted to length -1 with nothing else written for it; memory outside the given tensors is never touched. */
+typedef struct {
+    int pages, page, max_pages, max_len;
+    void *K, *V;
+    float *Ks, *Vs;
+    const int* table;
+    int* lengths;             /* [B] device; written by csat_cache_evict to its destination only */
+} csat_cache;
+
+/* Stores the packed rows of K and V (float or bf16, k_offsets, n_k, max_k as above) as the last tokens of their
+ * sequences: lengths[b] counts them already.  A block gets the smallest scale 2^e, e >= -118, with every finite |x| <= 448 * 2^e;
+ * where a block holds older tokens its scale only grows, and theirs are rounded anew to it (exact but for values that
+ * fall below 2^-6 of the new scale).  A non-finite x is stored as NaN and does not count for the scale.  Slots
+ * beyond the length keep what they held.  Each page written to must belong to one sequence only. */
+csat_status csat_cache_store(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* K, const void* V,
+                             const int* k_offsets, void* stream);
+
+/* Attention of packed rows Q over the cache (n_q, max_q, q_offsets; n_k, max_k, K's and V's strides are not used): with
+ * causal, row i of a sequence's n rows sees the first lengths[b] - n + i + 1 tokens, so that n = 1 is a decode step and n
+ * > 1 its last n tokens; 0: all of them.  O, lse as above; a NaN among the tokens that a row does not see has no effect on it.
+ * W (float [B, Hkv, max_pages * page], optional): W[b, h, t] = decay * W[b, h, t] + the weights that the rows and the
+ * heads of the group gave token t, t < lengths[b]; 0 <= decay <= 1, with 0 W is written, not read.
+ * Workspace: csat_cache_workspace_bytes (host-only query for these dims and this cache; it may be 0). */
+csat_status csat_cache_workspace_bytes(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes);
+csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* Q,
+                                 const int* q_offsets, float scale, float decay, void* O, float* lse, float* W,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Cuts every sequence of `from` down to budget >= 1 tokens per head: the last `recent` (0 <= recent <= budget) stay, and of the
+ * others those with the largest W (NaN counts as the largest, ties go to the lowest slot).  What stays is copied in its
+ * order to the pages of `to` (which must be none of the pages read; their pools may be the same, page sizes must be), blocks with
+ * the smallest scale for what they hold; W_to [B, Hkv, to->max_pages * page] gets their weights,
+ * kept [B, Hkv, budget] int32 their slots in `from` (-1 behind them), to->lengths their number.  Every head keeps tokens of its own.
+ * to->max_len and to->max_pages * page must be at least min(budget, from->max_len), else CSAT_ERR_SHAPE. */
+csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat_cache* from, const csat_cache* to,
+                             const float* W, float* W_to, int budget, int recent, int* kept, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------
  * Everything below this line is benchmark instrumentation and reference kernels: not part of the method,
  * not needed by a user of the block.
  * ------------------------------------------------------------------------------------------------------ */
@@ -257,7 +335,11 @@ typedef enum {
     CSAT_K_RESIDUAL = 5,   /* ISTA: r = y - Phi x */
     CSAT_K_UPDATE = 6,     /* ISTA: x <- eta(x + mu Phi^T r) */
     CSAT_K_SYNTHESIS = 7,  /* C^ = X V */
-    CSAT_K_COUNT = 8
+    CSAT_K_PROMPT = 8,     /* exact attention over packed sequences */
+    CSAT_K_STORE = 9,      /* cache: new tokens */
+    CSAT_K_CACHED = 10,    /* cache: attention over it */
+    CSAT_K_EVICT = 11,     /* cache: eviction */
+    CSAT_K_COUNT = 12
 } csat_kernel_id;
 csat_status csat_profile_enable(void* ctx, int on);
 csat_status csat_profile_read(void* ctx, int kernel_id, double* total_ms, int* launches);
@@ -278,7 +360,8 @@ typedef enum {
     CSAT_FORM_OMP_REFIT = 6,         /* matching pursuit's orthonormal vectors: 1 held in registers, 2 stored */
     CSAT_FORM_RESIDUAL = 7,          /* large-tile decoder's residual: parts of the product along K, 16 more where its kernel over the support is a launch of its own */
     CSAT_FORM_SCREEN_TILE = 8,       /* rows left out, bf16: columns of a tile of the product that finds them (256 or 320), 0 where none was looked for */
-    CSAT_FORM_COUNT = 9
+    CSAT_FORM_KEY_SHARES = 9,        /* exact attention, attention over the cache: shares of a sequence's keys, joined by a second launch */
+    CSAT_FORM_COUNT = 10
 } csat_launch_form;
 csat_status csat_profile_launch_form(void* ctx, int form, int* value);
 

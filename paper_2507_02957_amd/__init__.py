@@ -23,6 +23,7 @@ EXPORTS = (
     "csat_recover_hadamard", "csat_measure_hadamard", "csat_forward_hadamard", "csat_forward_rd_hadamard", "csat_measure_kv", "csat_forward_kv", "csat_forward_rd_kv",
     "csat_peak_copy", "csat_peak_mfma", "csat_peak_mfma_issue", "csat_profile_enable", "csat_profile_read", "csat_profile_decoder_kernel", "csat_profile_launch_form",
     "csat_set_option", "csat_decoder_status", "csat_static_workspace_bytes", "csat_forward_static",
+    "csat_prompt_workspace_bytes", "csat_prompt_attention", "csat_cache_store", "csat_cache_workspace_bytes", "csat_cache_attention", "csat_cache_evict",
 )
 # keys of csat_set_option (include/csat.h, csat_option)
 OPTIONS = {"decoder": 0, "gemm": 1, "raster": 2, "state": 3, "fused_segments": 4, "fused_thin": 5, "lista": 6,
@@ -30,15 +31,27 @@ OPTIONS = {"decoder": 0, "gemm": 1, "raster": 2, "state": 3, "fused_segments": 4
            "measure": 12, "synthesis": 13, "y_layout": 14, "support": 15, "screen": 16}
 # forms of csat_profile_launch_form (include/csat.h, csat_launch_form)
 LAUNCH_FORMS = {"decoder_members": 0, "small_tiles": 1, "attention_waves": 2, "lista_tile": 3, "omp_shares": 4, "omp_pick": 5, "omp_refit": 6,
-                "residual": 7, "screen_tile": 8}
+                "residual": 7, "screen_tile": 8, "key_shares": 9}
 CSAT_ERR_TIMEOUT = -8
 KERNEL_IDS = {"layout": 0, "measure": 1, "scores": 2, "softmax": 3, "output": 4, "residual": 5, "update": 6,
               "synthesis": 7}
+# ... and those of the exact attention and its cache, which are no stages of the block
+ATTENTION_KERNEL_IDS = {"prompt": 8, "store": 9, "cached": 10, "evict": 11}
 
 
 class csat_dims(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("n_q", ctypes.c_int), ("n", ctypes.c_int),
                 ("d", ctypes.c_int), ("m", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class csat_packed_dims(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("B", "Hq", "Hkv", "d", "n_q", "n_k", "max_q", "max_k", "causal", "dtype")] + \
+        [(name, ctypes.c_longlong) for name in ("q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "o_token", "o_head")]
+
+
+class csat_cache(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("pages", "page", "max_pages", "max_len")] + \
+        [(name, ctypes.c_void_p) for name in ("K", "V", "Ks", "Vs", "table", "lengths")]
 
 
 class CsatError(RuntimeError):
@@ -96,6 +109,13 @@ def load_library() -> ctypes.CDLL:
     lib.csat_profile_read.argtypes = [vp, it, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(it)]
     lib.csat_profile_decoder_kernel.argtypes = [vp, ctypes.POINTER(it)]
     lib.csat_profile_launch_form.argtypes = [vp, it, ctypes.POINTER(it)]
+    pp, cp = ctypes.POINTER(csat_packed_dims), ctypes.POINTER(csat_cache)
+    lib.csat_prompt_workspace_bytes.argtypes = [pp, ctypes.POINTER(sz)]
+    lib.csat_prompt_attention.argtypes = [vp, pp, vp, vp, vp, vp, vp, fl, vp, vp, vp, sz, vp]
+    lib.csat_cache_store.argtypes = [vp, pp, cp, vp, vp, vp, vp]
+    lib.csat_cache_workspace_bytes.argtypes = [pp, cp, ctypes.POINTER(sz)]
+    lib.csat_cache_attention.argtypes = [vp, pp, cp, vp, vp, fl, fl, vp, vp, vp, vp, sz, vp]
+    lib.csat_cache_evict.argtypes = [vp, pp, cp, cp, vp, vp, it, it, vp, vp]
     for name in EXPORTS:
         if name != "csat_status_string":
             getattr(lib, name).restype = it
@@ -117,13 +137,45 @@ def context() -> ctypes.c_void_p:
     return _ctx
 
 
-def make_dims(B, H, n_q, n, d, m, dtype) -> csat_dims:
-    """dtype: CSAT_F32 / CSAT_BF16, "f32" / "bf16", or a torch dtype."""
+def _dtype_code(dtype) -> int:
     code = {"f32": CSAT_F32, "bf16": CSAT_BF16, CSAT_F32: CSAT_F32, CSAT_BF16: CSAT_BF16}.get(dtype)
     if code is None:
         import torch
         code = {torch.float32: CSAT_F32, torch.bfloat16: CSAT_BF16}[dtype]
-    return csat_dims(B, H, n_q, n, d, m, code)
+    return code
+
+
+def make_dims(B, H, n_q, n, d, m, dtype) -> csat_dims:
+    """dtype: CSAT_F32 / CSAT_BF16, "f32" / "bf16", or a torch dtype."""
+    return csat_dims(B, H, n_q, n, d, m, _dtype_code(dtype))
+
+
+def make_packed_dims(B, Hq, Hkv, d, n_q, n_k, max_q, max_k, dtype, causal=True, Q=None, K=None, V=None, O=None) -> csat_packed_dims:
+    """Packed rows [n, heads, d] (dtype as in make_dims).  A tensor given for Q, K, V or O, with these three axes and its features
+    next to each other, brings its strides; without one the rows are contiguous."""
+    def strides(t, heads):
+        if t is None:
+            return heads * d, d
+        if t.stride(2) != 1:
+            raise ValueError("the features of a row must be next to each other")
+        return t.stride(0), t.stride(1)
+    return csat_packed_dims(B, Hq, Hkv, d, n_q, n_k, max_q, max_k, int(bool(causal)), _dtype_code(dtype), *strides(Q, Hq), *strides(K, Hkv),
+                            *strides(V, Hkv), *strides(O, Hq))
+
+
+def make_cache(K, V, Ks, Vs, table, lengths, max_len=None) -> csat_cache:
+    """K: codes [pages, Hkv, page, d], V: [pages, Hkv, d, page] (one byte each, e.g. torch.float8_e4m3fn), Ks, Vs: float32
+    [pages, Hkv], table: int32 [B, max_pages], lengths: int32 [B], all contiguous; max_len: the longest length (default: what the
+    table has room for).  The structure holds the tensors' addresses and keeps them alive."""
+    pages, _, page, _ = K.shape
+    for t in (K, V, Ks, Vs, table, lengths):
+        if not t.is_contiguous():
+            raise ValueError("the tensors of a cache are contiguous")
+    max_pages = table.shape[1]
+    c = csat_cache(pages, page, max_pages, max_pages * page if max_len is None else max_len, K.data_ptr(), V.data_ptr(), Ks.data_ptr(),
+                   Vs.data_ptr(), table.data_ptr(), lengths.data_ptr())
+    c.tensors = (K, V, Ks, Vs, table, lengths)
+    return c
 
 
 def _ptr(t):
@@ -315,6 +367,52 @@ def csat_forward_static(dims, Q, K, V, Phi, lam, step, iters, C, Z, X, stream=No
                                               lam, step, iters, _ptr(C), _ptr(Z), _ptr(X), _stream(stream)))
 
 
+def _on_device_of(t, stream, call):
+    """call(stream pointer) with t's device current (None: that device's current stream)."""
+    import torch
+    if t.device.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(t.device):
+        return call(_stream(stream))
+
+
+def csat_prompt_workspace_bytes(dims: csat_packed_dims) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().csat_prompt_workspace_bytes(ctypes.byref(dims), ctypes.byref(out)))
+    return out.value
+
+
+def csat_prompt_attention(dims, Q, K, V, q_offsets, k_offsets, scale, O, lse, workspace, stream=None):
+    """q_offsets, k_offsets: int32 device tensors [B + 1]; lse: float32 [Hq, n_q] or None; workspace may be None where none is needed."""
+    _check(_on_device_of(Q, stream, lambda st: load_library().csat_prompt_attention(
+        context(), ctypes.byref(dims), _ptr(Q), _ptr(K), _ptr(V), _ptr(q_offsets), _ptr(k_offsets), scale, _ptr(O), _ptr(lse), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), st)))
+
+
+def csat_cache_store(dims, cache, K, V, k_offsets, stream=None):
+    _check(_on_device_of(K, stream, lambda st: load_library().csat_cache_store(
+        context(), ctypes.byref(dims), ctypes.byref(cache), _ptr(K), _ptr(V), _ptr(k_offsets), st)))
+
+
+def csat_cache_workspace_bytes(dims: csat_packed_dims, cache: csat_cache) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().csat_cache_workspace_bytes(ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(out)))
+    return out.value
+
+
+def csat_cache_attention(dims, cache, Q, q_offsets, scale, decay, O, lse, W, workspace, stream=None):
+    """lse: float32 [Hq, n_q] or None; W: float32 [B, Hkv, max_pages * page] or None."""
+    _check(_on_device_of(Q, stream, lambda st: load_library().csat_cache_attention(
+        context(), ctypes.byref(dims), ctypes.byref(cache), _ptr(Q), _ptr(q_offsets), scale, decay, _ptr(O), _ptr(lse), _ptr(W), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), st)))
+
+
+def csat_cache_evict(dims, cache, to, W, W_to, budget, recent, kept, stream=None):
+    """kept: int32 [B, Hkv, budget]; to.lengths is written."""
+    _check(_on_device_of(W, stream, lambda st: load_library().csat_cache_evict(
+        context(), ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(to), _ptr(W), _ptr(W_to), budget, recent, _ptr(kept), st)))
+
+
 def csat_profile_enable(on: bool):
     _check(load_library().csat_profile_enable(context(), int(bool(on))))
 
@@ -337,5 +435,6 @@ def csat_profile_launch_form(form: str) -> int:
 def csat_profile_read(kernel: str):
     """(total milliseconds, launches) recorded for one step since profiling was enabled."""
     ms, cnt = ctypes.c_double(), ctypes.c_int()
-    _check(load_library().csat_profile_read(context(), KERNEL_IDS[kernel], ctypes.byref(ms), ctypes.byref(cnt)))
+    kid = {**KERNEL_IDS, **ATTENTION_KERNEL_IDS}[kernel]
+    _check(load_library().csat_profile_read(context(), kid, ctypes.byref(ms), ctypes.byref(cnt)))
     return ms.value, cnt.value

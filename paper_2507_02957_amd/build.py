@@ -35,6 +35,8 @@ UNITS = [(f"ista_resident_{mt}_{c}", "csat_tu_ista_resident.hip", [f"-DCSAT_TU_M
 UNITS += [("ista_resident_f32", "csat_tu_ista_resident_f32.hip", [])]
 UNITS += [("attention_z", "csat_tu_attention_z.hip", [])]
 UNITS += [("support", "csat_tu_support.hip", [])]
+UNITS += [(f"prompt_{'bf16' if b else 'f32'}", "csat_tu_prompt.hip", [f"-DCSAT_TU_BF16={b}"]) for b in (1, 0)]
+UNITS += [("cache", "csat_tu_cache.hip", [])]
 SOURCES = sorted({os.path.join(CSRC, src) for _, src, _ in UNITS})
 
 

@@ -15,6 +15,7 @@
 #include "csat_measure.h"
 #include "csat_support.h"
 #include "csat_screen.h"
+#include "csat_cache.h"
 #include "csat_launch.h"
 #include "csat_peaks.h"
 
@@ -354,7 +355,8 @@ bool decoder_is_resident_f32(const csat_dims& d, const Workspace& w, int iters) 
 
 struct Timed {   // brackets the launches issued during its lifetime
     Profiler* p; hipStream_t st;
-    Timed(const Workspace& w, int kid, hipStream_t s) : p(w.prof), st(s) { p->begin(kid, st); }
+    Timed(const Workspace& w, int kid, hipStream_t s) : Timed(w.prof, kid, s) {}
+    Timed(Profiler* prof, int kid, hipStream_t s) : p(prof), st(s) { p->begin(kid, st); }
     ~Timed() { p->end(st); }
 };
 
@@ -2166,6 +2168,74 @@ bool hadamard_fits_lds(int n, int m) {
     return need <= kLdsPerWorkgroup;
 }
 
+// ---- Exact attention over packed sequences and the 8-bit cache (csat_prompt.h, csat_cache.h)
+
+constexpr long long kMaxGrid = 0x7fffffffLL;
+constexpr long long kMaxTokenStride = 1 << 24;
+
+bool stride_ok(long long token, long long head, size_t e) {
+    return token >= 0 && token < kMaxTokenStride && head >= 0 && token * (long long)e % 16 == 0 && head * (long long)e % 16 == 0;
+}
+csat_status check_packed(const csat_packed_dims* d, int d_multiple) {
+    if (!d) return CSAT_ERR_NULL;
+    if (d->dtype != CSAT_F32 && d->dtype != CSAT_BF16) return CSAT_ERR_DTYPE;
+    if (d->B <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->d <= 0 || d->n_q <= 0 || d->n_k <= 0 || d->max_q <= 0 || d->max_k <= 0) return CSAT_ERR_SHAPE;
+    if (d->Hq % d->Hkv != 0 || d->d % d_multiple != 0 || d->d > 256) return CSAT_ERR_SHAPE;
+    if ((long long)d->B * d->Hq > 0xffffffLL || (long long)d->n_q * d->Hq > kMaxGrid) return CSAT_ERR_SHAPE;
+    return CSAT_OK;
+}
+// max_q, max_k beyond the packed rows say nothing more
+int longest_q(const csat_packed_dims& d) { return std::min(d.max_q, d.n_q); }
+int longest_k(const csat_packed_dims& d) { return std::min(d.max_k, d.n_k); }
+
+struct PromptPlan { int tiles, shares; size_t bytes; };
+// Row tiles of 128; the keys in shares where the tiles leave most of the chip idle, a share no shorter than 256 keys.
+PromptPlan prompt_plan(const csat_packed_dims& d) {
+    PromptPlan p{};
+    const int G = d.Hq / d.Hkv;
+    const long long rows = (long long)longest_q(d) * G;
+    p.tiles = (int)((rows + 127) / 128);
+    const long long groups = (long long)d.B * d.Hkv * p.tiles;
+    p.shares = (int)std::max(1LL, std::min<long long>(512 / groups, longest_k(d) / 256));
+    p.bytes = p.shares > 1 ? (size_t)p.shares * d.n_q * d.Hq * (d.d + 2) * 4 : 0;
+    return p;
+}
+
+csat_status check_cache(const csat_packed_dims& d, const csat_cache* c) {
+    if (!c) return CSAT_ERR_NULL;
+    if (c->pages <= 0 || c->max_pages <= 0 || c->max_len <= 0) return CSAT_ERR_SHAPE;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return CSAT_ERR_SHAPE;
+    if ((long long)c->max_pages * c->page < c->max_len || (long long)c->max_pages * c->page > kMaxGrid) return CSAT_ERR_SHAPE;
+    if ((long long)d.B * d.Hkv * ((c->max_len + c->page - 1) / c->page) > kMaxGrid) return CSAT_ERR_SHAPE;
+    return CSAT_OK;
+}
+csat_status check_cache_pointers(const csat_cache& c) {
+    if (!c.K || !c.V || !c.Ks || !c.Vs || !c.table || !c.lengths) return CSAT_ERR_NULL;
+    if (!aligned16(c.K) || !aligned16(c.V) || !aligned16(c.Ks) || !aligned16(c.Vs) || !aligned16(c.table) || !aligned16(c.lengths)) return CSAT_ERR_ALIGN;
+    return CSAT_OK;
+}
+CacheView cache_view(const csat_cache& c) {
+    CacheView v{};
+    v.K = (uint8_t*)c.K; v.V = (uint8_t*)c.V; v.Ks = c.Ks; v.Vs = c.Vs; v.table = c.table; v.lengths = c.lengths;
+    v.pages = c.pages; v.page = c.page; v.max_pages = c.max_pages; v.max_len = c.max_len;
+    for (v.log_page = 4; (1 << v.log_page) < c.page; ++v.log_page) {}
+    return v;
+}
+
+struct CachedPlan { int tiles, shares, score_ld; size_t part_bytes, bytes; };
+// The tokens in shares until there are four workgroups for every compute unit, a share no shorter than 512 tokens.
+CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weights) {
+    CachedPlan p{};
+    const long long rows = (long long)longest_q(d) * (d.Hq / d.Hkv);
+    p.tiles = (int)((rows + 15) / 16);
+    const long long groups = (long long)d.B * d.Hkv * p.tiles;
+    p.shares = (int)std::max(1LL, std::min<long long>(1024 / groups, c.max_len / 512));
+    p.score_ld = (int)round_up(c.max_len, 64);
+    p.part_bytes = p.shares > 1 || weights ? (size_t)round_up((long long)p.shares * d.n_q * d.Hq * (d.d + 2) * 4, 256) : 0;
+    p.bytes = p.part_bytes + (weights ? (size_t)d.B * d.Hkv * rows * p.score_ld * 4 : 0);
+    return p;
+}
+
 // Scratch of csat_forward_static: the workspace of a small problem, held in the code object's own device memory
 // so that the call allocates nothing.  Every device the library is used on holds its own copy until the process ends.
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
@@ -2727,6 +2797,144 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
     hipStream_t st = (hipStream_t)stream;
     return DISPATCH(*dims, forward_t<float>(*dims, w, Q, K, V, Phi, Phi, lambda, step, iters, C, Z, X, st),
                     forward_t<bf16_t>(*dims, w, Q, K, V, Phi, Phi, lambda, step, iters, C, Z, X, st));
+}
+
+csat_status csat_prompt_workspace_bytes(const csat_packed_dims* dims, size_t* bytes) {
+    CSAT_TRY(check_packed(dims, 8));
+    if (!bytes) return CSAT_ERR_NULL;
+    *bytes = prompt_plan(*dims).bytes;
+    return CSAT_OK;
+}
+
+csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const void* Q, const void* K, const void* V,
+                                  const int* q_offsets, const int* k_offsets, float scale, void* O, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+    CSAT_TRY(check_ctx(ctx));
+    CSAT_TRY(check_packed(dims, 8));
+    const csat_packed_dims& d = *dims;
+    const size_t e = esize(d.dtype);
+    if (!Q || !K || !V || !q_offsets || !k_offsets || !O) return CSAT_ERR_NULL;
+    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.k_token, d.k_head, e) || !stride_ok(d.v_token, d.v_head, e) || !stride_ok(d.o_token, d.o_head, e))
+        return CSAT_ERR_SHAPE;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return CSAT_ERR_PARAM;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_offsets) || !aligned16(k_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace))
+        return CSAT_ERR_ALIGN;
+    const PromptPlan p = prompt_plan(d);
+    if ((long long)d.B * d.Hkv * p.tiles * p.shares > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
+    OptionScope scope(ctx);
+    hipStream_t st = (hipStream_t)stream;
+    PromptArgs a{};
+    a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = lse; a.q_off = q_offsets; a.k_off = k_offsets;
+    a.q_token = d.q_token; a.q_head = d.q_head; a.k_token = d.k_token; a.k_head = d.k_head;
+    a.v_token = d.v_token; a.v_head = d.v_head; a.o_token = d.o_token; a.o_head = d.o_head;
+    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.d = d.d; a.n_q = d.n_q; a.n_k = d.n_k; a.max_q = longest_q(d); a.causal = d.causal != 0;
+    a.sl = scale * 1.4426950408889634f;
+    a.tiles = p.tiles; a.shares = p.shares; a.part = (float*)workspace;
+    Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_PROMPT, st);
+    HIP_TRY(d.dtype == CSAT_BF16 ? prompt_launch_bf16(a, st) : prompt_launch_f32(a, st));
+    if (p.shares > 1) {
+        tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares};
+        HIP_TRY(d.dtype == CSAT_BF16 ? attention_join_launch_bf16(j, st) : attention_join_launch_f32(j, st));
+    }
+    return CSAT_OK;
+}
+
+csat_status csat_cache_store(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* K, const void* V,
+                             const int* k_offsets, void* stream) {
+    CSAT_TRY(check_ctx(ctx));
+    CSAT_TRY(check_packed(dims, 16));
+    const csat_packed_dims& d = *dims;
+    CSAT_TRY(check_cache(d, cache));
+    CSAT_TRY(check_cache_pointers(*cache));
+    if (!K || !V || !k_offsets) return CSAT_ERR_NULL;
+    const size_t e = esize(d.dtype);
+    if (!stride_ok(d.k_token, d.k_head, e) || !stride_ok(d.v_token, d.v_head, e)) return CSAT_ERR_SHAPE;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(k_offsets)) return CSAT_ERR_ALIGN;
+    OptionScope scope(ctx);
+    hipStream_t st = (hipStream_t)stream;
+    StoreArgs a{};
+    a.c = cache_view(*cache);
+    a.K = K; a.V = V; a.k_off = k_offsets;
+    a.k_token = d.k_token; a.k_head = d.k_head; a.v_token = d.v_token; a.v_head = d.v_head;
+    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.n_k = d.n_k; a.max_k = longest_k(d);
+    a.reach = std::min((a.max_k - 1 + cache->page - 1) / cache->page + 1, (cache->max_len + cache->page - 1) / cache->page);
+    Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_STORE, st);
+    HIP_TRY(cache_store_launch(d.dtype == CSAT_BF16, a, st));
+    return CSAT_OK;
+}
+
+csat_status csat_cache_workspace_bytes(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes) {
+    CSAT_TRY(check_packed(dims, 16));
+    CSAT_TRY(check_cache(*dims, cache));
+    if (!bytes) return CSAT_ERR_NULL;
+    *bytes = cached_plan(*dims, *cache, true).bytes;
+    return CSAT_OK;
+}
+
+csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* Q,
+                                 const int* q_offsets, float scale, float decay, void* O, float* lse, float* W,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    CSAT_TRY(check_ctx(ctx));
+    CSAT_TRY(check_packed(dims, 16));
+    const csat_packed_dims& d = *dims;
+    CSAT_TRY(check_cache(d, cache));
+    CSAT_TRY(check_cache_pointers(*cache));
+    if (!Q || !q_offsets || !O) return CSAT_ERR_NULL;
+    const size_t e = esize(d.dtype);
+    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.o_token, d.o_head, e)) return CSAT_ERR_SHAPE;
+    if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
+    if (!aligned16(Q) || !aligned16(q_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(W) || !aligned16(workspace)) return CSAT_ERR_ALIGN;
+    const CachedPlan p = cached_plan(d, *cache, W != nullptr);
+    if ((long long)d.B * d.Hkv * p.tiles * p.shares > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
+    OptionScope scope(ctx);
+    hipStream_t st = (hipStream_t)stream;
+    CachedArgs a{};
+    a.c = cache_view(*cache);
+    a.Q = Q; a.O = O; a.lse = lse; a.q_off = q_offsets;
+    a.q_token = d.q_token; a.q_head = d.q_head; a.o_token = d.o_token; a.o_head = d.o_head;
+    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.d = d.d; a.n_q = d.n_q; a.max_q = longest_q(d); a.causal = d.causal != 0;
+    a.sl = scale * 1.4426950408889634f;
+    a.tiles = p.tiles; a.shares = p.shares;
+    a.part = p.part_bytes ? (float*)workspace : nullptr;
+    a.scores = W ? (float*)((char*)workspace + p.part_bytes) : nullptr;
+    a.score_ld = p.score_ld; a.W = W; a.decay = decay;
+    Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_CACHED, st);
+    HIP_TRY(cache_attention_launch(d.dtype == CSAT_BF16, a, st));
+    if (a.part) {
+        tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares};
+        HIP_TRY(d.dtype == CSAT_BF16 ? attention_join_launch_bf16(j, st) : attention_join_launch_f32(j, st));
+        if (W) HIP_TRY(cache_weights_launch(a, st));
+    }
+    return CSAT_OK;
+}
+
+csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat_cache* from, const csat_cache* to,
+                             const float* W, float* W_to, int budget, int recent, int* kept, void* stream) {
+    CSAT_TRY(check_ctx(ctx));
+    CSAT_TRY(check_packed(dims, 16));
+    const csat_packed_dims& d = *dims;
+    CSAT_TRY(check_cache(d, from));
+    CSAT_TRY(check_cache(d, to));
+    CSAT_TRY(check_cache_pointers(*from));
+    CSAT_TRY(check_cache_pointers(*to));
+    if (!W || !W_to || !kept) return CSAT_ERR_NULL;
+    if (budget < 1 || recent < 0 || recent > budget) return CSAT_ERR_PARAM;
+    const int most = std::min(budget, from->max_len);
+    if (from->page != to->page || to->max_len < most || (long long)d.B * d.Hkv * budget > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (!aligned16(W) || !aligned16(W_to) || !aligned16(kept)) return CSAT_ERR_ALIGN;
+    OptionScope scope(ctx);
+    hipStream_t st = (hipStream_t)stream;
+    EvictArgs a{};
+    a.from = cache_view(*from); a.to = cache_view(*to);
+    a.W = W; a.W_to = W_to; a.kept = kept;
+    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.budget = budget; a.recent = recent;
+    Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_EVICT, st);
+    HIP_TRY(cache_evict_launch(a, (most + from->page - 1) / from->page, st));
+    return CSAT_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,685 @@
+// Key/value cache in 8 bits: store, attention over it, eviction.
+//
+// A block is one page of one head: `page` tokens of e4m3 codes under one scale 2^e.  With a power of two, x / scale and a
+// code brought to another scale are exact before their one rounding to e4m3, so store and eviction have one right answer, bit
+// for bit, and a code that keeps its scale keeps its bits.
+//
+// K lies [token][d] and V [d][token] within a block: what a lane of the attention's matrix instructions needs, 16 features
+// of a token of K and 16 tokens of a feature of V, is 16 consecutive bytes of memory in either, so the attention reads
+// the cache straight into registers, without LDS and without a transposition.
+#pragma once
+#include "csat_prompt.h"
+
+namespace csat {
+
+struct CacheView {
+    uint8_t *K, *V;
+    float *Ks, *Vs;
+    const int* table;
+    int* lengths;
+    int pages, page, log_page, max_pages, max_len;
+};
+
+constexpr int kScaleMin = -118;
+// 2^e, |e| <= 126
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// smallest e >= kScaleMin with amax <= 448 * 2^e = 0.875 * 2^(e + 9), of a finite amax >= 0
+__device__ __forceinline__ int scale_exponent(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    const int e = (int)(u >> 23) - 126 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0) - 9;      // amax = f 2^(u >> 23) - 126), f in [0.5, 1)
+    return e < kScaleMin ? kScaleMin : e;                                                // (a subnormal amax is far below the least scale)
+}
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23) - 127; }
+
+__device__ __forceinline__ float finite_abs(float x) {
+    const float v = fabsf(x);
+    return v < INFINITY ? v : 0.f;
+}
+__device__ __forceinline__ float nan_if_odd(float x) { return fabsf(x) < INFINITY ? x : __uint_as_float(0x7fc00000u); }
+// four floats (already divided by the scale) -> four codes, nearest, ties to even
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_odd(a), nan_if_odd(b), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_odd(c), nan_if_odd(d), w, true);
+    return (uint32_t)w;
+}
+__device__ __forceinline__ uint32_t rescale_codes(uint32_t w, float f) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return to_codes(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+}
+
+// ---- store
+
+struct StoreArgs {
+    CacheView c;
+    const void *K, *V;
+    const int* k_off;
+    long long k_token, k_head, v_token, v_head;
+    int B, Hkv, d, n_k, max_k, reach;      // reach: pages that one sequence's new tokens may touch
+};
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) x = fmaxf(x, __shfl_xor(x, s));
+    return x;
+}
+
+// One workgroup per touched block (K and V of it).  Two passes over its new rows, the second of which finds them in the
+// cache: the largest finite magnitudes, then the codes.
+template <typename T>
+__global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
+    __shared__ float red[2][4];
+    const int tid = threadIdx.x;
+    const int hk = blockIdx.x % a.Hkv, i = blockIdx.x / a.Hkv % a.reach, b = blockIdx.x / a.Hkv / a.reach;
+    const PackedSpan ks(a.k_off, b, a.n_k);
+    const int n = ks.count < a.max_k ? ks.count : a.max_k;
+    const int len = a.c.lengths[b];
+    if (n <= 0 || len > a.c.max_len || len < n) return;
+    const int start = len - n, page = a.c.page, first = start >> a.c.log_page, last = (len - 1) >> a.c.log_page;
+    const int j = first + i;
+    if (j > last) return;
+    // a sequence with a page that does not exist is not stored to at all
+    bool bad = false;
+    for (int t = first + tid; t <= last; t += 256) {
+        const int p = a.c.table[(long long)b * a.c.max_pages + t];
+        bad |= p < 0 || p >= a.c.pages;
+    }
+    if (__syncthreads_or(bad)) return;
+    const int id = a.c.table[(long long)b * a.c.max_pages + j];
+    const int lo = j == first ? start - j * page : 0, hi = j == last ? len - j * page : page;      // new slots
+    const long long row0 = ks.first + ((long long)j * page - start);      // packed row of slot 0
+    const T* K = (const T*)a.K + row0 * a.k_token + (long long)hk * a.k_head;
+    const T* V = (const T*)a.V + row0 * a.v_token + (long long)hk * a.v_head;
+    const long long block = (long long)id * a.Hkv + hk;
+    uint8_t* const ck = a.c.K + block * page * a.d;
+    uint8_t* const cv = a.c.V + block * page * a.d;
+
+    const int dq = a.d / 4;                 // pieces of four features
+    float mk = 0.f, mv = 0.f;
+    auto four = [](const T* p, float* x) {
+        if constexpr (sizeof(T) == 2) {
+            const uint2 w = *(const uint2*)p;
+            x[0] = __uint_as_float(w.x << 16); x[1] = __uint_as_float(w.x & 0xffff0000u);
+            x[2] = __uint_as_float(w.y << 16); x[3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+            const float4 w = *(const float4*)p;
+            x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
+        }
+    };
+    for (int q = tid; q < (hi - lo) * dq; q += 256) {
+        const int s = lo + q / dq, f = q % dq * 4;
+        float x[4];
+        four(K + (long long)s * a.k_token + f, x);
+        mk = fmaxf(mk, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
+        four(V + (long long)s * a.v_token + f, x);
+        mv = fmaxf(mv, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
+    }
+    mk = wave_max(mk);
+    mv = wave_max(mv);
+    if ((tid & 63) == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
+    const float ok = lo ? a.c.Ks[block] : 0.f, ov = lo ? a.c.Vs[block] : 0.f;
+    __syncthreads();
+    mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    const float sk = fmaxf(pow2f(scale_exponent(mk)), ok), sv = fmaxf(pow2f(scale_exponent(mv)), ov);
+    if (tid == 0) { a.c.Ks[block] = sk; a.c.Vs[block] = sv; }
+    const float ik = pow2f(-exponent_of(sk)), iv = pow2f(-exponent_of(sv));
+
+    for (int q = tid; q < (hi - lo) * dq; q += 256) {
+        const int s = lo + q / dq, f = q % dq * 4;
+        float x[4];
+        four(K + (long long)s * a.k_token + f, x);
+        *(uint32_t*)(ck + (long long)s * a.d + f) = to_codes(x[0] * ik, x[1] * ik, x[2] * ik, x[3] * ik);
+    }
+    if (lo && sk != ok) {
+        const float f = ok * ik;
+        for (int q = tid; q < lo * dq; q += 256) ((uint32_t*)ck)[q] = rescale_codes(((uint32_t*)ck)[q], f);
+    }
+    // V: a thread takes one feature of sixteen tokens
+    const int groups = page / 16;
+    for (int q = tid; q < groups * a.d; q += 256) {
+        const int f = q % a.d, g = q / a.d * 16;
+        if (g >= hi || (g + 16 <= lo && sv == ov)) continue;
+        uint8_t* const out = cv + (long long)f * page + g;
+        uint4 w = uint4{0u, 0u, 0u, 0u};
+        const bool whole = g >= lo && g + 16 <= hi;
+        if (!whole) w = *(const uint4*)out;
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) {
+            float x[4];
+            uint32_t keep = 0;      // bytes of this word that are old or behind the new ones
+            const uint32_t was = (&w.x)[k / 4];
+            uint32_t old = was;
+            if (sv != ov && g + k < lo) old = rescale_codes(was, ov * iv);
+            uint32_t mix = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int s = g + k + e;
+                x[e] = 0.f;
+                if (s < lo) { keep |= 0xffu << (8 * e); mix |= old & (0xffu << (8 * e)); }
+                else if (s >= hi) { keep |= 0xffu << (8 * e); mix |= was & (0xffu << (8 * e)); }
+                else x[e] = Elem<T>::load(V + (long long)s * a.v_token + f) * iv;
+            }
+            (&w.x)[k / 4] = (to_codes(x[0], x[1], x[2], x[3]) & ~keep) | mix;
+        }
+        *(uint4*)out = w;
+    }
+}
+
+// ---- attention over the cache
+
+struct CachedArgs {
+    CacheView c;
+    const void* Q;
+    void* O;
+    float* lse;
+    const int* q_off;
+    long long q_token, q_head, o_token, o_head;
+    int B, Hq, Hkv, G, d, n_q, max_q, causal;
+    float sl;                      // scale log2(e)
+    int tiles;                     // 16-row tiles per sequence and key head
+    int shares;                    // workgroups that split a sequence's tokens
+    float* part;                   // [shares][n_q Hq][d], then [shares][n_q Hq][2] as in csat_prompt.h, or null: O and lse are written
+    float* scores;                 // [B][Hkv][max_q G][score_ld] in units of log2, for the weights, or null
+    int score_ld;
+    float* W;                      // [B][Hkv][max_pages page]
+    float decay;
+};
+
+__device__ __forceinline__ float quad_max(float x) {      // over lanes n, n + 16, n + 32, n + 48
+    const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_max(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_sum(__uint_as_float(sw[0]) + __uint_as_float(sw[1]));
+}
+// eight codes -> a bf16 fragment (every e4m3 value is a bf16 value)
+__device__ __forceinline__ bf16x8 code_fragment(uint32_t lo, uint32_t hi) {
+    uint4 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }      // a byte's top bit: it is NaN
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+    const uint32_t n = nan_codes(w);
+    return w & ~((n - (n >> 7)) | n);
+}
+__device__ __forceinline__ uint32_t one_where_nan(uint32_t w) { return (nan_codes(w) >> 7) * 0x38u; }      // 0x38: 1.0
+
+// A tile is 64 tokens by 16 rows.  S^T = K Q^T with 16 x 16 x 32 instructions: instruction row i of sub-tile s is token
+// 16 (i / 4) + 4 s + i % 4, so that a lane's 16 scores are those of the 16 consecutive tokens 16 quad .. + 15 of one query
+// row, and, as the B operand of O^T = V^T P^T, meet 16 consecutive bytes of V^T.  A wavefront takes every fourth tile of its
+// share and keeps a running maximum and sum of its own; the four are joined through LDS at the end.
+template <typename T, int DC>
+__global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
+    constexpr int NP = sizeof(T) == 2 ? 1 : 3;      // float queries and weights as three bf16 parts: 24 bits
+    constexpr int DT = 4 * DC;
+    extern __shared__ float joint[];                // [4][16][d + 4] outputs, then [4][16][2]
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hk = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv % a.tiles, share = blockIdx.x / a.Hkv / a.tiles % a.shares;
+    const int b = blockIdx.x / a.Hkv / a.tiles / a.shares;
+    const PackedSpan qs(a.q_off, b, a.n_q);
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G, r_base = 16 * tile;
+    if (r_base >= rows) return;
+    int L = a.c.lengths[b];
+    bool bad = L < 0 || L > a.c.max_len;
+    if (bad) L = 0;
+    auto limit_of = [&](int r) {
+        if (!a.causal) return L;
+        const int v = r / a.G + L - qs.count + 1;
+        return v < 0 ? 0 : v > L ? L : v;
+    };
+    const int r_last = r_base + 16 < rows ? r_base + 15 : rows - 1;
+    const int lo = limit_of(r_base), hi = limit_of(r_last);
+    const int steps = (hi + 63) / 64;
+    const int t0 = (int)((long long)steps * share / a.shares), t1 = (int)((long long)steps * (share + 1) / a.shares);
+    const int r = r_base + li < rows ? r_base + li : rows - 1;
+    const int tok = r / a.G, head = hk * a.G + r % a.G, lim = limit_of(r);
+
+    // features 64 c + 16 quad + 8 h .. + 7 of the lane's row
+    bf16x8 qf[NP][DC][2];
+    {
+        const T* q = (const T*)a.Q + (long long)(qs.first + tok) * a.q_token + (long long)head * a.q_head;
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int f = 64 * c + 16 * quad + 8 * h;
+                if constexpr (NP == 1) {
+                    qf[0][c][h] = __builtin_bit_cast(bf16x8, f < a.d ? *(const uint4*)(q + f) : uint4{0u, 0u, 0u, 0u});
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float x = f < a.d ? ((const float*)q)[f + e] : 0.f;
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            qf[p][c][h][e] = (__bf16)x;
+                            x -= (float)qf[p][c][h][e];
+                        }
+                    }
+                }
+            }
+    }
+    f32x4 o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float ref = -INFINITY, sum = 0.f;
+
+    const int page = a.c.page, lp = a.c.log_page, last_page = (L - 1) >> lp;
+    const int* const table = a.c.table + (long long)b * a.c.max_pages;
+    const long long head_bytes = (long long)page * a.d;
+    auto page_of = [&](int t) {      // (a token behind the last: any page that exists, masked below)
+        int i = t >> lp;
+        i = i < last_page ? i : last_page;
+        int id = table[i];
+        if (id < 0 || id >= a.c.pages) { bad = true; id = 0; }
+        return id;
+    };
+    for (int t = t0 + wave; t < t1; t += 4) {
+        const int first = 64 * t;
+        const int kt = first + 16 * (li >> 2), vt = first + 16 * quad;
+        const int kid = page_of(kt), vid = page_of(vt);
+        const uint8_t* kp = a.c.K + ((long long)kid * a.Hkv + hk) * head_bytes + (long long)((kt & (page - 1)) + (li & 3)) * a.d + 16 * quad;
+        const uint8_t* vp = a.c.V + ((long long)vid * a.Hkv + hk) * head_bytes + (long long)li * page + (vt & (page - 1));
+        const float kscale = a.c.Ks[(long long)vid * a.Hkv + hk] * a.sl, vscale = a.c.Vs[(long long)vid * a.Hkv + hk];
+        uint4 kw[4][DC], vw[DT];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int c = 0; c < DC; ++c) kw[s][c] = 64 * c + 16 * quad < a.d ? *(const uint4*)(kp + (long long)(4 * s) * a.d + 64 * c) : uint4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int u = 0; u < DT; ++u) vw[u] = 16 * u < a.d ? *(const uint4*)(vp + (long long)(16 * u) * page) : uint4{0u, 0u, 0u, 0u};
+
+        float e[16];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < DC; ++c) {
+                const bf16x8 k0 = code_fragment(kw[s][c].x, kw[s][c].y), k1 = code_fragment(kw[s][c].z, kw[s][c].w);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[p][c][0], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[p][c][1], acc, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[4 * s + i] = acc[i] * kscale;
+        }
+        const bool masks = first + 64 > lo;
+        if (masks) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (vt + i >= lim) e[i] = -INFINITY;
+        }
+        if (a.scores && r_base + li < rows) {
+            float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G + r) * a.score_ld + vt;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[i], e[i + 1], e[i + 2], e[i + 3]};
+        }
+        float mx = e[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, e[i]);
+        mx = quad_max(mx);
+        if (__builtin_amdgcn_ballot_w64(mx - ref > 8.f) != 0) {
+            const float nm = fmaxf(mx, ref);
+            const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - nm);
+            ref = nm;
+            sum *= f;
+#pragma unroll
+            for (int u = 0; u < DT; ++u) o[u] *= f;
+        }
+        const float base = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(e[i] - base);
+            sum += e[i];
+            e[i] *= vscale;
+        }
+        // weights of bf16 precision for bf16 tensors; the other parts for float ones
+        bf16x8 pf[NP][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float x = e[8 * h + i];
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    pf[p][h][i] = (__bf16)x;
+                    x -= (float)pf[p][h][i];
+                }
+            }
+        bool odd = false;
+        if (masks) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int u = 0; u < DT; ++u) any |= nan_codes(vw[u].x) | nan_codes(vw[u].y) | nan_codes(vw[u].z) | nan_codes(vw[u].w);
+            odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
+        }
+        if (odd) {      // a NaN reaches the rows that see its token: the others have weight 0 for it, and 0 times NaN is NaN
+            bf16x8 ones[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ones[h][i] = vt + 8 * h + i < lim ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+            for (int u = 0; u < DT; ++u) {
+                f32x4 cnt = f32x4{0.f, 0.f, 0.f, 0.f};
+                const uint4 w = vw[u];
+                cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(code_fragment(one_where_nan(w.x), one_where_nan(w.y)), ones[0], cnt, 0, 0, 0);
+                cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(code_fragment(one_where_nan(w.z), one_where_nan(w.w)), ones[1], cnt, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (cnt[i] > 0.f) o[u][i] = __uint_as_float(0x7fc00000u);
+                vw[u] = uint4{without_nan(w.x), without_nan(w.y), without_nan(w.z), without_nan(w.w)};
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < DT; ++u) {
+            const bf16x8 v0 = code_fragment(vw[u].x, vw[u].y), v1 = code_fragment(vw[u].z, vw[u].w);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                o[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[p][0], o[u], 0, 0, 0);
+                o[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[p][1], o[u], 0, 0, 0);
+            }
+        }
+    }
+
+    // the wavefronts' parts of a row, brought to the largest reference
+    const int pitch = a.d + 4;
+    float2* const ml = (float2*)(joint + 4 * 16 * pitch);
+    sum = quad_sum(sum);
+    if (__builtin_amdgcn_ballot_w64(bad) != 0) sum = __uint_as_float(0x7fc00000u);
+#pragma unroll
+    for (int u = 0; u < DT; ++u)
+        if (16 * u < a.d) *(f32x4*)(joint + (wave * 16 + li) * pitch + 16 * u + 4 * quad) = o[u];
+    if (quad == 0) ml[wave * 16 + li] = float2{ref, sum};
+    __syncthreads();
+    const int n_rows = rows - r_base < 16 ? rows - r_base : 16, dq = a.d / 4;
+    for (int q = tid; q < n_rows * dq; q += 256) {
+        const int i = q / dq, f = q % dq * 4;
+        float m = -INFINITY, total = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 16 + i].x);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 y = ml[w * 16 + i];
+            if (y.y == 0.f) continue;
+            const float k = y.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(y.x - m);      // (a sum that is NaN without a maximum stays)
+            const float4 z = *(const float4*)(joint + (w * 16 + i) * pitch + f);
+            total += k * y.y;
+            x[0] += k * z.x; x[1] += k * z.y; x[2] += k * z.z; x[3] += k * z.w;
+        }
+        const int rr = r_base + i, h = hk * a.G + rr % a.G;
+        const long long row = qs.first + rr / a.G;
+        if (a.part) {
+            const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + h;
+            *(float4*)(a.part + at * a.d + f) = float4{x[0], x[1], x[2], x[3]};
+            if (f == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[at] = float2{total == 0.f ? INFINITY : m == -INFINITY ? 0.f : -m, total};
+            continue;
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (a.lse && f == 0) a.lse[(long long)h * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) + m);
+        T* out = (T*)a.O + row * a.o_token + (long long)h * a.o_head + f;
+        if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(x[0] * inv, x[1] * inv), f2bf_pk(x[2] * inv, x[3] * inv)};
+        else *(float4*)out = float4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    }
+}
+
+// W = decay W + sum over rows of 2^(score - lse), a thread four tokens.
+static __global__ __launch_bounds__(256) void cache_weights_kernel(CachedArgs a) {
+    constexpr int RB = 64;
+    __shared__ float lse2[RB];
+    __shared__ int limit[RB];
+    const int tid = threadIdx.x;
+    const int chunks = (a.c.max_len + 1023) / 1024;
+    const int chunk = blockIdx.x % chunks, hk = blockIdx.x / chunks % a.Hkv, b = blockIdx.x / chunks / a.Hkv;
+    const int L = a.c.lengths[b], t = chunk * 1024 + 4 * tid;
+    if (L < 0 || L > a.c.max_len || chunk * 1024 >= L) return;
+    const PackedSpan qs(a.q_off, b, a.n_q);
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G;
+    const long long all = (long long)a.n_q * a.Hq;
+    const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d);
+    float* const w = a.W + ((long long)b * a.Hkv + hk) * a.c.max_pages * a.c.page + t;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < rows; r0 += RB) {
+        __syncthreads();
+        if (tid < RB && r0 + tid < rows) {
+            const int r = r0 + tid;
+            const long long at = (long long)(qs.first + r / a.G) * a.Hq + hk * a.G + r % a.G;
+            float off = INFINITY, total = 0.f;
+            for (int s = 0; s < a.shares; ++s) off = fminf(off, ml[(long long)s * all + at].x);
+            for (int s = 0; s < a.shares; ++s) {
+                const float2 y = ml[(long long)s * all + at];
+                if (y.x != INFINITY) total += __builtin_amdgcn_exp2f(off - y.x) * y.y;
+            }
+            lse2[tid] = total == 0.f ? INFINITY : __log2f(total) - off;      // (nothing seen: weights 0)
+            int v = a.causal ? r / a.G + L - qs.count + 1 : L;
+            limit[tid] = v < 0 ? 0 : v > L ? L : v;
+        }
+        __syncthreads();
+        const int n = rows - r0 < RB ? rows - r0 : RB;
+        if (t >= L) continue;
+        const float* s = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G + r0) * a.score_ld + t;
+        for (int i = 0; i < n; ++i, s += a.score_ld) {
+            const float4 y = *(const float4*)s;
+            const float l = lse2[i];
+            const int seen = limit[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (t + e < seen) x[e] += __builtin_amdgcn_exp2f((&y.x)[e] - l);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (t + e < L) w[e] = a.decay == 0.f ? x[e] : a.decay * w[e] + x[e];
+}
+
+// ---- eviction
+
+struct EvictArgs {
+    CacheView from, to;
+    const float* W;
+    float* W_to;
+    int* kept;
+    int B, Hkv, d, budget, recent;
+};
+
+constexpr int kSelectThreads = 1024;
+// Which tokens of a sequence and head stay: the least key that does, digit by digit from the highest (counts in LDS), then
+// one pass in slot order.  A key is a weight's bits in an order of whole numbers (NaN highest, -0 as 0).
+__device__ __forceinline__ uint32_t weight_key(float w) {
+    if (w != w) return 0xffffffffu;
+    const uint32_t u = __float_as_uint(w + 0.f);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictArgs a) {
+    constexpr int BINS = 2048, WAVES = kSelectThreads / 64;
+    __shared__ int bins[BINS];
+    __shared__ int wsum[WAVES][2];
+    __shared__ int found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
+    const int L = a.from.lengths[b], page = a.from.page;
+    int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget;
+    bool bad = L < 0 || L > a.from.max_len;
+    const int keep = bad ? 0 : L < a.budget ? L : a.budget;
+    if (!bad) {
+        for (int i = tid; i < (L + page - 1) / page; i += kSelectThreads) {
+            const int id = a.from.table[(long long)b * a.from.max_pages + i];
+            bad |= id < 0 || id >= a.from.pages;
+        }
+        for (int i = tid; i < (keep + page - 1) / page; i += kSelectThreads) {
+            const int id = a.to.table[(long long)b * a.to.max_pages + i];
+            bad |= id < 0 || id >= a.to.pages;
+        }
+    }
+    bad = __syncthreads_or(bad) != 0;
+    if (tid == 0 && hk == 0) a.to.lengths[b] = bad ? -1 : keep;
+    if (bad) {
+        for (int i = tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+        return;
+    }
+    for (int i = keep + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+    const float* const w = a.W + ((long long)b * a.Hkv + hk) * a.from.max_pages * page;
+    float* const w_to = a.W_to + ((long long)b * a.Hkv + hk) * a.to.max_pages * page;
+    const int recent = keep < a.recent ? keep : a.recent, n = L - recent, k = keep - recent;      // k of the first n
+    for (int i = tid; i < recent; i += kSelectThreads) {
+        kept[k + i] = n + i;
+        w_to[k + i] = w[n + i];
+    }
+    // the k-th largest key: prefix bits found so far, how many of the keys with that prefix still have to be taken
+    uint32_t prefix = 0;
+    int need = k;
+    if (k > 0 && k < n) {
+        int bits = 0;
+        for (int pass = 0; pass < 3; ++pass) {
+            const int width = pass < 2 ? 11 : 10, shift = 32 - bits - width;
+            for (int i = tid; i < BINS; i += kSelectThreads) bins[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < n; i += kSelectThreads) {
+                const uint32_t key = weight_key(w[i]);
+                if (bits == 0 || (key >> (32 - bits)) == prefix) atomicAdd(&bins[(key >> shift) & ((1u << width) - 1u)], 1);
+            }
+            __syncthreads();
+            if (wave == 0) {      // bins from the highest down: a lane sums 32 of them, then the lane that holds the place looks closer
+                const int per = (1 << width) / 64, top = (1 << width) - 1 - lane * per;
+                int mine = 0;
+                for (int i = 0; i < per; ++i) mine += bins[top - i];
+                int before = mine;
+#pragma unroll
+                for (int s = 1; s < 64; s *= 2) {
+                    const int y = __shfl_up(before, s);
+                    if (lane >= s) before += y;
+                }
+                before -= mine;
+                if (before < need && before + mine >= need) {
+                    int left = need - before, i = 0;
+                    while (bins[top - i] < left) { left -= bins[top - i]; ++i; }
+                    found[0] = top - i;
+                    found[1] = left;
+                }
+            }
+            __syncthreads();
+            prefix = (prefix << width) | (uint32_t)found[0];
+            need = found[1];
+            bits += width;
+            __syncthreads();
+        }
+    }
+    // in slot order: keys above the k-th, and the first `need` of those equal to it.  A wavefront takes a stretch of slots.
+    if (k <= 0) return;
+    const bool all = k >= n;
+    const int stretch = ((n + WAVES - 1) / WAVES + 63) / 64 * 64, s0 = wave * stretch, s1 = s0 + stretch < n ? s0 + stretch : n;
+    int above = 0, equal = 0;
+    for (int i0 = s0; i0 < s1; i0 += 64) {
+        const int i = i0 + lane;
+        const uint32_t key = i < s1 ? weight_key(w[i]) : 0;
+        const bool in = i < s1;
+        above += __popcll(__ballot(in && (all || key > prefix)));
+        equal += __popcll(__ballot(in && !all && key == prefix));
+    }
+    if (lane == 0) { wsum[wave][0] = above; wsum[wave][1] = equal; }
+    __syncthreads();
+    int at_above = 0, at_equal = 0;
+    for (int v = 0; v < wave; ++v) { at_above += wsum[v][0]; at_equal += wsum[v][1]; }
+    const unsigned long long below = (1ull << lane) - 1ull;
+    for (int i0 = s0; i0 < s1; i0 += 64) {
+        const int i = i0 + lane;
+        const bool in = i < s1;
+        const float x = in ? w[i] : 0.f;
+        const uint32_t key = weight_key(x);
+        const unsigned long long ma = __ballot(in && (all || key > prefix)), me = __ballot(in && !all && key == prefix);
+        const int ra = at_above + __popcll(ma & below), re = at_equal + __popcll(me & below);
+        const bool is_above = (ma >> lane) & 1, is_equal = (me >> lane) & 1;
+        if (is_above || (is_equal && re < need)) {
+            const int p = ra + (re < need ? re : need);
+            kept[p] = i;
+            w_to[p] = x;
+        }
+        at_above += __popcll(ma);
+        at_equal += __popcll(me);
+    }
+}
+
+// One workgroup per destination block: gathers its tokens' codes of K and V, each under its source's scale, and rounds them to
+// the block's own.
+static __global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a, int blocks) {
+    __shared__ long long src_block[128];      // page * Hkv + head
+    __shared__ int src_slot[128];
+    __shared__ float src_k[128], src_v[128];
+    __shared__ float red[2][4];
+    const int tid = threadIdx.x, page = a.from.page, d = a.d;
+    const int hk = blockIdx.x % a.Hkv, j = blockIdx.x / a.Hkv % blocks, b = blockIdx.x / a.Hkv / blocks;
+    const int keep = a.to.lengths[b];
+    if (j * page >= keep) return;             // (-1: nothing)
+    const int n = keep - j * page < page ? keep - j * page : page;
+    const int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget + (long long)j * page;
+    for (int i = tid; i < n; i += 256) {
+        const int t = kept[i];
+        const long long block = (long long)a.from.table[(long long)b * a.from.max_pages + (t >> a.from.log_page)] * a.Hkv + hk;
+        src_block[i] = block;
+        src_slot[i] = t & (page - 1);
+        src_k[i] = a.from.Ks[block];
+        src_v[i] = a.from.Vs[block];
+    }
+    __syncthreads();
+    const long long size = (long long)page * d, dst = (long long)a.to.table[(long long)b * a.to.max_pages + j] * a.Hkv + hk;
+    // magnitudes: a code's low seven bits are in the order of the values, NaN (0x7f) above all
+    auto largest = [](uint32_t w) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t c = (w >> (8 * e)) & 0x7fu;
+            m = c != 0x7fu && c > m ? c : m;
+        }
+        return m;
+    };
+    auto value = [](uint32_t c) { return (float)__builtin_amdgcn_cvt_pk_f32_fp8((int)c, false)[0]; };
+    const int dq = d / 4, groups = (n + 3) / 4;
+    float mk = 0.f, mv = 0.f;
+    for (int q = tid; q < n * dq; q += 256) {
+        const int i = q / dq, f = q % dq * 4;
+        mk = fmaxf(mk, value(largest(*(const uint32_t*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f))) * src_k[i]);
+    }
+    for (int q = tid; q < d * n; q += 256) {
+        const int i = q % n, f = q / n;
+        mv = fmaxf(mv, value(largest(a.from.V[src_block[i] * size + (long long)f * page + src_slot[i]])) * src_v[i]);
+    }
+    mk = wave_max(mk);
+    mv = wave_max(mv);
+    if ((tid & 63) == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
+    __syncthreads();
+    mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
+    const int ek = scale_exponent(mk), ev = scale_exponent(mv);
+    if (tid == 0) { a.to.Ks[dst] = pow2f(ek); a.to.Vs[dst] = pow2f(ev); }
+    const float ik = pow2f(-ek), iv = pow2f(-ev);
+    for (int q = tid; q < n * dq; q += 256) {
+        const int i = q / dq, f = q % dq * 4;
+        const uint32_t w = *(const uint32_t*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f);
+        const float s = src_k[i] * ik;
+        *(uint32_t*)(a.to.K + dst * size + (long long)i * d + f) = s == 1.f ? w : rescale_codes(w, s);
+    }
+    for (int q = tid; q < d * groups; q += 256) {
+        const int g = q % groups * 4, f = q / groups;
+        uint32_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = g + e < n ? g + e : n - 1;
+            const uint32_t c = a.from.V[src_block[i] * size + (long long)f * page + src_slot[i]];
+            const float s = src_v[i] * iv;
+            w |= (s == 1.f ? c : rescale_codes(c, s) & 0xffu) << (8 * e);
+        }
+        uint8_t* const out = a.to.V + dst * size + (long long)f * page + g;
+        if (g + 4 <= n) *(uint32_t*)out = w;
+        else
+            for (int e = 0; g + e < n; ++e) out[e] = (uint8_t)(w >> (8 * e));
+    }
+}
+
+}  // namespace csat

@@ -12,6 +12,11 @@ struct IstaResidentF32Args;
 struct AttentionArgs;
 struct AttentionZArgs;
 struct ListaSupportArgs;
+struct PromptArgs;
+struct JoinArgs;
+struct StoreArgs;
+struct CachedArgs;
+struct EvictArgs;
 
 // Fused ISTA decoder for MT tiles of m (csat_ista_fused.h, csat_ista_fused2.h).  variant: 0 dense state, 1 sparse
 // state, 2 one 32-row tile per workgroup (thin); 3 and 4: dense and sparse state on the two-chunk schedule; 6:
@@ -54,5 +59,18 @@ hipError_t attention_z_launch(int d, int parts, bool resident, const AttentionZA
 // The unrolled decoder over the support of its iterate (csat_support.h), n <= kListaSupportMaxN, a workgroup per four rows.
 constexpr int kListaSupportMaxN = 4096;
 hipError_t lista_support_launch(const ListaSupportArgs& a, unsigned grid, hipStream_t st);
+
+// Exact attention over packed sequences (csat_prompt.h), and the join of the shares of its keys; csat_tu_prompt.hip compiled
+// with -DCSAT_TU_BF16=<0|1>.
+hipError_t prompt_launch_bf16(const PromptArgs& a, hipStream_t st);
+hipError_t prompt_launch_f32(const PromptArgs& a, hipStream_t st);
+hipError_t attention_join_launch_bf16(const JoinArgs& a, hipStream_t st);
+hipError_t attention_join_launch_f32(const JoinArgs& a, hipStream_t st);
+
+// The 8-bit cache (csat_cache.h).  blocks: the most that a sequence and head has after an eviction.
+hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st);
+hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st);
+hipError_t cache_weights_launch(const CachedArgs& a, hipStream_t st);
+hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st);
 
 }  // namespace csat

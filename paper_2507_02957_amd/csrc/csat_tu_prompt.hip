@@ -1,0 +1,39 @@
+// Translation unit of the exact attention over packed sequences for one element type: compile with -DCSAT_TU_BF16=<0|1>.
+#include "csat_prompt.h"
+#include "csat_launch.h"
+
+#ifndef CSAT_TU_BF16
+#error "compile with -DCSAT_TU_BF16=<0|1>"
+#endif
+
+namespace csat {
+
+#if CSAT_TU_BF16
+typedef bf16_t T;
+#define CSAT_TU_FN(name) name##_bf16
+#else
+typedef float T;
+#define CSAT_TU_FN(name) name##_f32
+#endif
+
+hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, hipStream_t st) {
+    auto launch = [&](auto kernel, int lds_bytes) -> hipError_t {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.B * a.Hkv * a.tiles * a.shares)), dim3(64 * kPromptWaves), lds_bytes, st, a);
+        return hipGetLastError();
+    };
+#define CSAT_PROMPT(DT_) launch(prompt_kernel<T, DT_, 1>, prompt_lds_bytes<T, DT_>())
+    if (a.d <= 64) return CSAT_PROMPT(2);
+    if (a.d <= 96) return CSAT_PROMPT(3);
+    if (a.d <= 128) return CSAT_PROMPT(4);
+    return CSAT_PROMPT(8);
+#undef CSAT_PROMPT
+}
+
+hipError_t CSAT_TU_FN(attention_join_launch)(const JoinArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)(a.B * (((long long)a.max_q * a.Hq + 3) / 4))), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace csat

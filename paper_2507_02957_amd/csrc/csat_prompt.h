@@ -30,7 +30,9 @@ struct PromptArgs {
 
 constexpr int kPromptWaves = 4;
 template <typename T> constexpr int prompt_key_tiles() { return sizeof(T) == 2 ? 2 : 1; }      // 32-key tiles per step
-template <typename T, int DT> constexpr int prompt_lds_bytes() { return 2 * 2 * prompt_key_tiles<T>() * 32 * DT * 32 * (int)sizeof(T); }
+template <typename T, int DT> constexpr int prompt_lds_bytes() {
+    return 2 * 2 * prompt_key_tiles<T>() * 32 * DT * 32 * (int)sizeof(T) + 32 * DT * 12 + 16;      // K and V twice; three keys a column, a word
+}
 
 // One sequence's rows: clamped to the tensors whatever the offsets say.
 struct PackedSpan {
@@ -44,37 +46,47 @@ struct PackedSpan {
     }
 };
 
-// Values of a 16-byte piece that are infinite or NaN.
-template <typename T> __device__ __forceinline__ bool not_finite(const uint4& w);
-template <> __device__ __forceinline__ bool not_finite<bf16_t>(const uint4& w) {
-    bool any = false;
+// Infinities and NaN in V where some row does not see their key: a weight of 0 times one of them is NaN.  They are taken out
+// of the staged tile (only a step with a masked key is looked through) and noted per column, the lowest key of each kind; at
+// the end a row that sees that key, as rows see a leading part of the keys, gets what the sum would have been.
+struct OddColumn { int nan, pinf, ninf; };
+constexpr int kNoKey = 0x7fffffff;
+template <typename T> __device__ __forceinline__ uint32_t odd_values(const uint4& w);      // bit e: value e of the piece
+template <> __device__ __forceinline__ uint32_t odd_values<bf16_t>(const uint4& w) {
+    uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t x = (&w.x)[i];
-        any |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+        m |= ((x & 0x7f80u) == 0x7f80u ? 1u : 0u) << (2 * i) | ((x & 0x7f800000u) == 0x7f800000u ? 1u : 0u) << (2 * i + 1);
     }
-    return any;
+    return m;
 }
-template <> __device__ __forceinline__ bool not_finite<float>(const uint4& w) {
-    bool any = false;
+template <> __device__ __forceinline__ uint32_t odd_values<float>(const uint4& w) {
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) any |= ((&w.x)[i] & 0x7f800000u) == 0x7f800000u;
-    return any;
+    for (int i = 0; i < 4; ++i) m |= (((&w.x)[i] & 0x7f800000u) == 0x7f800000u ? 1u : 0u) << i;
+    return m;
 }
-// A fragment dword of bf16 pairs: what is finite; and 1.0 where it is NaN (kind 0), +inf (1), -inf (2).
-__device__ __forceinline__ uint32_t finite_pair(uint32_t x) {
-    return x & (((x & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u));
+template <typename T>
+__device__ __forceinline__ uint4 take_odd(uint4 w, int key, OddColumn* col, int* any) {
+    const uint32_t m = odd_values<T>(w);
+    if (m == 0) return w;
+    *any = 1;
+    constexpr int EPC = Elem<T>::per_chunk;
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) {
+        if (!((m >> e) & 1)) continue;
+        uint32_t& word = (&w.x)[e * (int)sizeof(T) / 4];
+        const float x = sizeof(T) == 2 ? __uint_as_float(e & 1 ? word & 0xffff0000u : word << 16) : __uint_as_float(word);
+        word &= sizeof(T) == 4 ? 0u : e & 1 ? 0xffffu : 0xffff0000u;
+        atomicMin(x != x ? &col[e].nan : x > 0.f ? &col[e].pinf : &col[e].ninf, key);
+    }
+    return w;
 }
-__device__ __forceinline__ uint32_t odd_pair(uint32_t x, int kind) {
-    auto one = [&](uint32_t v) -> uint32_t {
-        const bool is = kind == 0 ? (v & 0x7fffu) > 0x7f80u : v == (kind == 1 ? 0x7f80u : 0xff80u);
-        return is ? 0x3f80u : 0u;
-    };
-    return one(x & 0xffffu) | (one(x >> 16) << 16);
-}
-__device__ __forceinline__ float odd_value(float finite, float nan, float pinf, float ninf) {
-    if (nan > 0.f || (pinf > 0.f && ninf > 0.f)) return __uint_as_float(0x7fc00000u);
-    return pinf > 0.f ? finite + INFINITY : ninf > 0.f ? finite - INFINITY : finite;
+__device__ __forceinline__ float with_odd(float finite, const OddColumn& c, int limit) {
+    const bool p = c.pinf < limit, n = c.ninf < limit;
+    if (c.nan < limit || (p && n)) return __uint_as_float(0x7fc00000u);
+    return p ? finite + INFINITY : n ? finite - INFINITY : finite;
 }
 
 __device__ __forceinline__ float pair_max(float x) {
@@ -86,20 +98,29 @@ __device__ __forceinline__ float pair_sum(float x) {
     return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
 }
 
+// Swizzles of the staged tiles: 16-byte piece c of row `row` lies at piece c ^ swizzle, C pieces a row, so that 16 rows' pieces of
+// K (one fragment read), or 4 rows' 64 bytes of V (half a transposing read; float: 2 rows 4 apart), cover the 64 banks once.
+template <int C> __device__ __forceinline__ int swizzle_k(int row) { return C % 16 == 0 ? row & 15 : C % 8 == 0 ? (row >> 1) & 7 : (row >> 2) & 3; }
+template <typename T, int C> __device__ __forceinline__ int swizzle_v(int row) {
+    if (sizeof(T) == 4) return C % 16 == 0 ? 8 * ((row >> 2) & 1) : 0;
+    return C % 16 == 0 ? 4 * (row & 3) : C % 8 == 0 ? 4 * ((row >> 1) & 1) : 0;
+}
+
 template <typename T, int DT, int NT>
-__global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a) {
+__global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+    typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
+    typedef __attribute__((address_space(3))) const float* lds_float;
     constexpr bool BF = sizeof(T) == 2;
     constexpr int KT = prompt_key_tiles<T>(), KEYS = 32 * KT, D = 32 * DT, THREADS = 64 * kPromptWaves;
     constexpr int EPC = Elem<T>::per_chunk, C = D / EPC, NK = C / 2;      // 16-byte pieces of a row, pairs of them
-    constexpr int PIECES = KEYS * C / THREADS;
+    constexpr int PIECES = KEYS * C / THREADS, TILE = KEYS * C * 16;
     static_assert(KEYS * C % THREADS == 0, "a step's pieces are dealt out evenly");
-    // swizzles within a row: 8 rows (K, read 16 bytes per row) or 4 rows (V, read 32 bytes per row) fall into different banks
-    constexpr int SWK = C % 8 == 0 ? 7 : 3, SWV = C % 8 == 0 ? 3 : 1;
-    extern __shared__ uint4 lds[];
-    uint4* const ldsK = lds;
-    uint4* const ldsV = lds + 2 * KEYS * C;
+    extern __shared__ uint4 lds[];                  // K tile, V tile; the same once more; then the columns' odd values
+    OddColumn* const oddc = (OddColumn*)(lds + 4 * KEYS * C);
+    int* const any_odd = (int*)(oddc + D);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
 
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -128,17 +149,15 @@ __global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a)
     const bool active = w_base < rows;
     const int w_end = w_base + 32 * NT < rows ? w_base + 32 * NT : rows;
     const int w_lo = active ? limit_of(w_base) : 0, w_hi = active ? limit_of(w_end - 1) : 0;
-    int lim[NT], tok[NT], head[NT];
+    int lim[NT];
     uint4 qf[NT][NK];
     const int dc = a.d / EPC;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         int r = w_base + 32 * n + li;
         if (r >= rows) r = rows - 1;
-        tok[n] = r / a.G;
-        head[n] = hk * a.G + r % a.G;
         lim[n] = limit_of(r);
-        const T* q = (const T*)a.Q + (long long)(qs.first + tok[n]) * a.q_token + (long long)head[n] * a.q_head;
+        const T* q = (const T*)a.Q + (long long)(qs.first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
 #pragma unroll
         for (int g = 0; g < NK; ++g) {
             const int c = 2 * g + lh;
@@ -155,39 +174,64 @@ __global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a)
 #pragma unroll
             for (int v = 0; v < 16; ++v) o[n][t][v] = 0.f;
     }
+    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
+    if (tid == 0) *any_odd = 0;
 
-    const T* const kb = (const T*)a.K + (long long)ks.first * a.k_token + (long long)hk * a.k_head;
-    const T* const vb = (const T*)a.V + (long long)ks.first * a.v_token + (long long)hk * a.v_head;
+    // A step's pieces: base of the step, the same for all threads, and a piece's place within it (token strides are below 2^24
+    // elements, so 32 bits hold it).  Rows behind the sequence's last one as that one (masked), columns behind d as zeros.
+    const char* const kb = (const char*)a.K + ((long long)ks.first * a.k_token + (long long)hk * a.k_head) * (long long)sizeof(T);
+    const char* const vb = (const char*)a.V + ((long long)ks.first * a.v_token + (long long)hk * a.v_head) * (long long)sizeof(T);
+    const long long k_step = (long long)KEYS * a.k_token * (long long)sizeof(T), v_step = (long long)KEYS * a.v_token * (long long)sizeof(T);
     uint4 kr[PIECES], vr[PIECES];
-    auto load = [&](int t) {      // rows behind the sequence's last one as that one (masked), columns behind d as zeros
+    uint32_t ko[PIECES], vo[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+        const int q = p * THREADS + tid, row = q / C, c = q % C;
+        ko[p] = ((uint32_t)row * (uint32_t)a.k_token + c * EPC) * (uint32_t)sizeof(T);
+        vo[p] = ((uint32_t)row * (uint32_t)a.v_token + c * EPC) * (uint32_t)sizeof(T);
+        kr[p] = vr[p] = uint4{0u, 0u, 0u, 0u};
+    }
+    auto load = [&](int t) {
+        const char* const kt = kb + t * k_step;
+        const char* const vt = vb + t * v_step;
+        if (dc == C && (t + 1) * KEYS <= nk) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                kr[p] = *(const uint4*)(kt + ko[p]);
+                vr[p] = *(const uint4*)(vt + vo[p]);
+            }
+            return;
+        }
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
             const int q = p * THREADS + tid, c = q % C;
-            int row = t * KEYS + q / C;
-            row = row < nk ? row : nk - 1;
-            kr[p] = vr[p] = uint4{0u, 0u, 0u, 0u};
+            const int row = t * KEYS + q / C < nk ? q / C : nk - 1 - t * KEYS;
             if (c < dc) {
-                kr[p] = *(const uint4*)(kb + (long long)row * a.k_token + c * EPC);
-                vr[p] = *(const uint4*)(vb + (long long)row * a.v_token + c * EPC);
+                kr[p] = *(const uint4*)(kt + ((long long)row * a.k_token + c * EPC) * (long long)sizeof(T));
+                vr[p] = *(const uint4*)(vt + ((long long)row * a.v_token + c * EPC) * (long long)sizeof(T));
             }
         }
     };
     if (t0 < t1) load(t0);
+    __syncthreads();                                 // (the columns' odd values are set up)
     for (int t = t0; t < t1; ++t) {
-        uint4* const sk = ldsK + (t & 1) * KEYS * C;
-        uint4* const sv = ldsV + (t & 1) * KEYS * C;
-        const bool masks = (t + 1) * KEYS > lo;      // some row of the workgroup does not see all of the step's keys
-        bool odd = false;
+        const uint32_t sk = lds0 + (t & 1) * 2 * TILE, sv = sk + TILE;
+        uint4* const wk = lds + (t & 1) * 2 * KEYS * C;
+        uint4* const wv = wk + KEYS * C;
+        if ((t + 1) * KEYS > lo) {                   // some row of the workgroup does not see all of the step's keys
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int q = p * THREADS + tid;
+                vr[p] = take_odd<T>(vr[p], t * KEYS + q / C, oddc + q % C * EPC, any_odd);
+            }
+        }
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
             const int q = p * THREADS + tid, row = q / C, c = q % C;
-            sk[row * C + (c ^ (row & SWK))] = kr[p];
-            sv[row * C + (c ^ (2 * (row & SWV)))] = vr[p];
-            if (masks) odd |= not_finite<T>(vr[p]);
+            wk[row * C + (c ^ swizzle_k<C>(row))] = kr[p];
+            wv[row * C + (c ^ swizzle_v<T, C>(row))] = vr[p];
         }
-        // (one barrier a step: the other half of the LDS was last read a step earlier)
-        if (masks) odd = __syncthreads_or(odd) != 0;
-        else __syncthreads();
+        __syncthreads();                             // (one barrier a step: the other half of the LDS was last read a step earlier)
         if (t + 1 < t1) load(t + 1);
         if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
 
@@ -202,12 +246,11 @@ __global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a)
         for (int g = 0; g < NK; ++g)
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
-                const uint4 kf = sk[(32 * u + li) * C + ((2 * g + lh) ^ (li & SWK))];
+                const u32x4 kf = *(lds_u32x4)(uintptr_t)(sk + (uint32_t)(((32 * u + li) * C + ((2 * g + lh) ^ swizzle_k<C>(li))) * 16));
 #pragma unroll
-                for (int n = 0; n < NT; ++n) mfma_group<T>(kf, qf[n][g], s[n][u]);
+                for (int n = 0; n < NT; ++n) mfma_group<T>(__builtin_bit_cast(uint4, kf), qf[n][g], s[n][u]);
             }
-        const bool w_masks = (t + 1) * KEYS > w_lo;
-        if (w_masks) {
+        if ((t + 1) * KEYS > w_lo) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -244,103 +287,65 @@ __global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a)
                     sum[n] += s[n][u][v];
                 }
         }
-        // O^T += V^T P^T.  A masked key's weight is 0, but 0 times an infinity or NaN is NaN: a step in which some row does not
-        // see all keys and V holds such a value takes the finite part of V, and the others by what they are, for the rows
-        // that see them (products with 1 for a visible key, 0 for a masked one).
-        auto product = [&](auto oddc) {
-            constexpr bool ODD = decltype(oddc)::value;
+        // O^T += V^T P^T
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                f32x16 cnt[ODD ? NT : 1][3];
-                if constexpr (ODD) {
+        for (int u = 0; u < KT; ++u) {
+            if constexpr (BF) {
+                const int l = lane & 15;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int h2 = 0; h2 < 2; ++h2) {
+                    uint4 pf[NT];
 #pragma unroll
-                        for (int k = 0; k < 3; ++k)
+                    for (int n = 0; n < NT; ++n) {
+                        const f32x16& e = s[n][u];
+                        pf[n] = uint4{f2bf_pk(e[8 * h2], e[8 * h2 + 1]), f2bf_pk(e[8 * h2 + 2], e[8 * h2 + 3]),
+                                      f2bf_pk(e[8 * h2 + 4], e[8 * h2 + 5]), f2bf_pk(e[8 * h2 + 6], e[8 * h2 + 7])};
+                    }
 #pragma unroll
-                            for (int v = 0; v < 16; ++v) cnt[n][k][v] = 0.f;
-                }
+                    for (int dt = 0; dt < DT; ++dt) {
+                        // rows 32 u + 16 h2 + 4 lh + {0..3} and the same + 8, columns 32 dt + 16 (lane / 16 % 2) + {0..15}
+                        const int row = 4 * lh + (l >> 2), c = 4 * dt + 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
+                        const uint32_t at0 = sv + (uint32_t)((row * C + (c ^ swizzle_v<T, C>(row))) * 16 + (l & 1) * 8);
+                        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at0 + (32 * u + 16 * h2) * C * 16));
+                        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at0 + (32 * u + 16 * h2 + 8) * C * 16));
+                        const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
 #pragma unroll
-                for (int u = 0; u < KT; ++u) {
-                    if constexpr (BF) {
-#pragma unroll
-                        for (int h2 = 0; h2 < 2; ++h2) {
-                            const int l = lane & 15;
-                            const int row = 32 * u + 16 * h2 + 4 * lh + (l >> 2);
-                            const int c = 4 * dt + 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
-                            const char* p = (const char*)(sv + row * C + (c ^ (2 * (row & SWV)))) + (l & 1) * 8;
-                            const char* p8 = (const char*)(sv + (row + 8) * C + (c ^ (2 * ((row + 8) & SWV)))) + (l & 1) * 8;
-                            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
-                            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p8);
-                            const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
-                            uint4 vf = uint4{w0.x, w0.y, w1.x, w1.y};
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) {
-                                const f32x16& e = s[n][u];
-                                const uint4 pf = uint4{f2bf_pk(e[8 * h2], e[8 * h2 + 1]), f2bf_pk(e[8 * h2 + 2], e[8 * h2 + 3]),
-                                                       f2bf_pk(e[8 * h2 + 4], e[8 * h2 + 5]), f2bf_pk(e[8 * h2 + 6], e[8 * h2 + 7])};
-                                if constexpr (ODD) {
-                                    uint4 fin, ones;
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        (&fin.x)[i] = finite_pair((&vf.x)[i]);
-                                        const int key = t * KEYS + 32 * u + 16 * h2 + 8 * (i >> 1) + 4 * lh + 2 * (i & 1);
-                                        (&ones.x)[i] = (key < lim[n] ? 0x3f80u : 0u) | (key + 1 < lim[n] ? 0x3f800000u : 0u);
-                                    }
-                                    mfma_group<T>(fin, pf, o[n][dt]);
-#pragma unroll
-                                    for (int k = 0; k < 3; ++k) {
-                                        uint4 ind;
-#pragma unroll
-                                        for (int i = 0; i < 4; ++i) (&ind.x)[i] = odd_pair((&vf.x)[i], k);
-                                        mfma_group<T>(ind, ones, cnt[n][k]);
-                                    }
-                                } else {
-                                    mfma_group<T>(vf, pf, o[n][dt]);
-                                }
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int row = 32 * u + 8 * (v >> 2) + 4 * lh + (v & 3), col = 32 * dt + li;
-                            const float x = ((const float*)(sv + row * C + ((col >> 2) ^ (2 * (row & SWV)))))[col & 3];
-#pragma unroll
-                            for (int n = 0; n < NT; ++n) {
-                                if constexpr (ODD) {
-                                    const bool fin = fabsf(x) < INFINITY;
-                                    const float one = t * KEYS + row < lim[n] ? 1.f : 0.f;
-                                    o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(fin ? x : 0.f, s[n][u][v], o[n][dt], 0, 0, 0);
-                                    cnt[n][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x != x ? 1.f : 0.f, one, cnt[n][0], 0, 0, 0);
-                                    cnt[n][1] = __builtin_amdgcn_mfma_f32_32x32x2f32(x == INFINITY ? 1.f : 0.f, one, cnt[n][1], 0, 0, 0);
-                                    cnt[n][2] = __builtin_amdgcn_mfma_f32_32x32x2f32(x == -INFINITY ? 1.f : 0.f, one, cnt[n][2], 0, 0, 0);
-                                } else {
-                                    o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[n][u][v], o[n][dt], 0, 0, 0);
-                                }
-                            }
-                        }
+                        for (int n = 0; n < NT; ++n) mfma_group<T>(uint4{w0.x, w0.y, w1.x, w1.y}, pf[n], o[n][dt]);
                     }
                 }
-                if constexpr (ODD) {
+            } else {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) o[n][dt][v] = odd_value(o[n][dt][v], cnt[n][0][v], cnt[n][1][v], cnt[n][2][v]);
-                }
+                    for (int v = 0; v < 16; ++v) {
+                        const int row = 4 * lh + (v & 3), c = 8 * dt + (li >> 2);
+                        const uint32_t at = sv + (uint32_t)((row * C + (c ^ swizzle_v<T, C>(row))) * 16 + (li & 3) * 4);
+                        const float x = *(lds_float)(uintptr_t)(at + (32 * u + 8 * (v >> 2)) * C * 16);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[n][u][v], o[n][dt], 0, 0, 0);
+                    }
             }
-        };
-        if (odd && w_masks) product(std::true_type{});
-        else product(std::false_type{});
+        }
     }
+    __syncthreads();                                 // (the last steps' odd values are noted)
     if (!active) return;
+    const bool odd = *any_odd != 0;
 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float total = pair_sum(sum[n]);
-        const bool ok = w_base + 32 * n + li < rows;
-        const long long row = qs.first + tok[n];
+        const int r = w_base + 32 * n + li;
+        const bool ok = r < rows;
+        const int rr = ok ? r : rows - 1, head = hk * a.G + rr % a.G;
+        const long long row = qs.first + rr / a.G;
+        if (odd) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[n][dt][v] = with_odd(o[n][dt][v], oddc[32 * dt + 8 * (v >> 2) + 4 * lh + (v & 3)], lim[n]);
+        }
         if (a.shares > 1) {
-            const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + head[n];
+            const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + head;
             if (ok) {
                 float* p = a.part + at * a.d;
 #pragma unroll
@@ -356,8 +361,8 @@ __global__ __launch_bounds__(64 * kPromptWaves) void prompt_kernel(PromptArgs a)
             continue;
         }
         const float inv = total == 0.f ? 0.f : 1.f / total;      // (a row that saw nothing is 0)
-        if (a.lse && ok && lh == 0) a.lse[(long long)head[n] * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off[n]);
-        T* out = (T*)a.O + row * a.o_token + (long long)head[n] * a.o_head;
+        if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off[n]);
+        T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll

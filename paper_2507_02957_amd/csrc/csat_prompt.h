@@ -68,25 +68,29 @@ template <> __device__ __forceinline__ uint32_t odd_values<float>(const uint4& w
     return m;
 }
 template <typename T>
-__device__ __forceinline__ uint4 take_odd(uint4 w, int key, OddColumn* col, int* any) {
+__device__ __forceinline__ void take_odd(uint4* piece, int key, OddColumn* col, int* any) {
+    const uint4 w = *piece;
     const uint32_t m = odd_values<T>(w);
-    if (m == 0) return w;
+    if (m == 0) return;
     *any = 1;
-    constexpr int EPC = Elem<T>::per_chunk;
-#pragma unroll
-    for (int e = 0; e < EPC; ++e) {
+    T* const x = (T*)piece;
+    for (int e = 0; e < Elem<T>::per_chunk; ++e) {
         if (!((m >> e) & 1)) continue;
-        uint32_t& word = (&w.x)[e * (int)sizeof(T) / 4];
-        const float x = sizeof(T) == 2 ? __uint_as_float(e & 1 ? word & 0xffff0000u : word << 16) : __uint_as_float(word);
-        word &= sizeof(T) == 4 ? 0u : e & 1 ? 0xffffu : 0xffff0000u;
-        atomicMin(x != x ? &col[e].nan : x > 0.f ? &col[e].pinf : &col[e].ninf, key);
+        const float v = Elem<T>::load(x + e);
+        atomicMin(v != v ? &col[e].nan : v > 0.f ? &col[e].pinf : &col[e].ninf, key);
+        Elem<T>::store(x + e, 0.f);
     }
-    return w;
 }
 __device__ __forceinline__ float with_odd(float finite, const OddColumn& c, int limit) {
     const bool p = c.pinf < limit, n = c.ninf < limit;
     if (c.nan < limit || (p && n)) return __uint_as_float(0x7fc00000u);
     return p ? finite + INFINITY : n ? finite - INFINITY : finite;
+}
+
+// 16 bytes of memory per lane, base + off, to LDS at `at` + 16 lane.  In assembly, so that the compiler, which cannot tell the half
+// that is written from the half that is read, does not wait for it before every LDS read: who calls it waits (vmcnt) himself.
+__device__ __forceinline__ void stage16(uint32_t at, const char* base, uint32_t off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(at), "v"(off), "s"(base) : "memory", "m0");
 }
 
 __device__ __forceinline__ float pair_max(float x) {
@@ -177,62 +181,56 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
     for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
     if (tid == 0) *any_odd = 0;
 
-    // A step's pieces: base of the step, the same for all threads, and a piece's place within it (token strides are below 2^24
-    // elements, so 32 bits hold it).  Rows behind the sequence's last one as that one (masked), columns behind d as zeros.
+    // A step's pieces go from memory straight into LDS, piece q of the tile at its place there; a thread's pieces q = 256 p + tid
+    // come from the places that the swizzles send there (token strides are below 2^24 elements, so 32 bits hold them within a
+    // step).  Rows behind the sequence's last one are that one again (masked); columns behind d are zeroed once and left out.
     const char* const kb = (const char*)a.K + ((long long)ks.first * a.k_token + (long long)hk * a.k_head) * (long long)sizeof(T);
     const char* const vb = (const char*)a.V + ((long long)ks.first * a.v_token + (long long)hk * a.v_head) * (long long)sizeof(T);
-    const long long k_step = (long long)KEYS * a.k_token * (long long)sizeof(T), v_step = (long long)KEYS * a.v_token * (long long)sizeof(T);
-    uint4 kr[PIECES], vr[PIECES];
+    const uint32_t k_row = (uint32_t)a.k_token * (uint32_t)sizeof(T), v_row = (uint32_t)a.v_token * (uint32_t)sizeof(T);
     uint32_t ko[PIECES], vo[PIECES];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
         const int q = p * THREADS + tid, row = q / C, c = q % C;
-        ko[p] = ((uint32_t)row * (uint32_t)a.k_token + c * EPC) * (uint32_t)sizeof(T);
-        vo[p] = ((uint32_t)row * (uint32_t)a.v_token + c * EPC) * (uint32_t)sizeof(T);
-        kr[p] = vr[p] = uint4{0u, 0u, 0u, 0u};
+        ko[p] = (uint32_t)row * k_row + 16u * (uint32_t)(c ^ swizzle_k<C>(row));
+        vo[p] = (uint32_t)row * v_row + 16u * (uint32_t)(c ^ swizzle_v<T, C>(row));
     }
+    if (dc < C)
+        for (int i = tid; i < 4 * KEYS * C; i += THREADS) lds[i] = uint4{0u, 0u, 0u, 0u};
     auto load = [&](int t) {
-        const char* const kt = kb + t * k_step;
-        const char* const vt = vb + t * v_step;
+        const char* const kt = kb + (long long)t * KEYS * k_row;
+        const char* const vt = vb + (long long)t * KEYS * v_row;
+        const uint32_t at = lds0 + (t & 1) * 2 * TILE + wave * 1024;
         if (dc == C && (t + 1) * KEYS <= nk) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                kr[p] = *(const uint4*)(kt + ko[p]);
-                vr[p] = *(const uint4*)(vt + vo[p]);
-            }
+            for (int p = 0; p < PIECES; ++p) stage16(at + p * THREADS * 16, kt, ko[p]);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) stage16(at + TILE + p * THREADS * 16, vt, vo[p]);
             return;
         }
+        const int left = nk - 1 - t * KEYS;
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int q = p * THREADS + tid, c = q % C;
-            const int row = t * KEYS + q / C < nk ? q / C : nk - 1 - t * KEYS;
-            if (c < dc) {
-                kr[p] = *(const uint4*)(kt + ((long long)row * a.k_token + c * EPC) * (long long)sizeof(T));
-                vr[p] = *(const uint4*)(vt + ((long long)row * a.v_token + c * EPC) * (long long)sizeof(T));
-            }
+            const int q = p * THREADS + tid, row = q / C, c = q % C, over = row > left ? row - left : 0;
+            if ((c ^ swizzle_k<C>(row)) < dc) stage16(at + p * THREADS * 16, kt, ko[p] - (uint32_t)over * k_row);
+            if ((c ^ swizzle_v<T, C>(row)) < dc) stage16(at + TILE + p * THREADS * 16, vt, vo[p] - (uint32_t)over * v_row);
         }
     };
+    __syncthreads();                                 // (the zeroed columns, and the columns' odd values are set up)
     if (t0 < t1) load(t0);
-    __syncthreads();                                 // (the columns' odd values are set up)
     for (int t = t0; t < t1; ++t) {
         const uint32_t sk = lds0 + (t & 1) * 2 * TILE, sv = sk + TILE;
-        uint4* const wk = lds + (t & 1) * 2 * KEYS * C;
-        uint4* const wv = wk + KEYS * C;
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this thread's pieces are there
+        __syncthreads();                             // ... and everybody's; the other half of the LDS has been read
+        if (t + 1 < t1) load(t + 1);
         if ((t + 1) * KEYS > lo) {                   // some row of the workgroup does not see all of the step's keys
+            uint4* const wv = lds + (t & 1) * 2 * KEYS * C + KEYS * C;
 #pragma unroll
             for (int p = 0; p < PIECES; ++p) {
-                const int q = p * THREADS + tid;
-                vr[p] = take_odd<T>(vr[p], t * KEYS + q / C, oddc + q % C * EPC, any_odd);
+                const int q = p * THREADS + tid, row = q / C, c = q % C ^ swizzle_v<T, C>(row);
+                take_odd<T>(wv + q, t * KEYS + row, oddc + c * EPC, any_odd);
             }
+            __syncthreads();
         }
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int q = p * THREADS + tid, row = q / C, c = q % C;
-            wk[row * C + (c ^ swizzle_k<C>(row))] = kr[p];
-            wv[row * C + (c ^ swizzle_v<T, C>(row))] = vr[p];
-        }
-        __syncthreads();                             // (one barrier a step: the other half of the LDS was last read a step earlier)
-        if (t + 1 < t1) load(t + 1);
         if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
 
         f32x16 s[NT][KT];

@@ -367,13 +367,23 @@ def csat_forward_static(dims, Q, K, V, Phi, lam, step, iters, C, Z, X, stream=No
                                               lam, step, iters, _ptr(C), _ptr(Z), _ptr(X), _stream(stream)))
 
 
-def _on_device_of(t, stream, call):
-    """call(stream pointer) with t's device current (None: that device's current stream)."""
+def _issue(entry, t, stream, args):
+    """Calls lib.<entry>(context, *args, stream) with tensor t's device current (stream None: that device's current stream).  A decode
+    step is a few microseconds on the GPU, so this is kept short: addresses go as plain integers, and the current stream's comes
+    without a stream object."""
     import torch
-    if t.device.index == torch.cuda.current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(t.device):
-        return call(_stream(stream))
+    index = t.device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return _issue(entry, t, stream, args)
+    st = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    status = getattr(_lib or load_library(), entry)(_ctx or context(), *args, st)
+    if status != 0:
+        _check(status)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def csat_prompt_workspace_bytes(dims: csat_packed_dims) -> int:
@@ -384,14 +394,13 @@ def csat_prompt_workspace_bytes(dims: csat_packed_dims) -> int:
 
 def csat_prompt_attention(dims, Q, K, V, q_offsets, k_offsets, scale, O, lse, workspace, stream=None):
     """q_offsets, k_offsets: int32 device tensors [B + 1]; lse: float32 [Hq, n_q] or None; workspace may be None where none is needed."""
-    _check(_on_device_of(Q, stream, lambda st: load_library().csat_prompt_attention(
-        context(), ctypes.byref(dims), _ptr(Q), _ptr(K), _ptr(V), _ptr(q_offsets), _ptr(k_offsets), scale, _ptr(O), _ptr(lse), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), st)))
+    _issue("csat_prompt_attention", Q, stream, (
+        ctypes.byref(dims), Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(), scale, O.data_ptr(), _at(lse),
+        _at(workspace), 0 if workspace is None else workspace.numel()))
 
 
 def csat_cache_store(dims, cache, K, V, k_offsets, stream=None):
-    _check(_on_device_of(K, stream, lambda st: load_library().csat_cache_store(
-        context(), ctypes.byref(dims), ctypes.byref(cache), _ptr(K), _ptr(V), _ptr(k_offsets), st)))
+    _issue("csat_cache_store", K, stream, (ctypes.byref(dims), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), k_offsets.data_ptr()))
 
 
 def csat_cache_workspace_bytes(dims: csat_packed_dims, cache: csat_cache) -> int:
@@ -402,15 +411,15 @@ def csat_cache_workspace_bytes(dims: csat_packed_dims, cache: csat_cache) -> int
 
 def csat_cache_attention(dims, cache, Q, q_offsets, scale, decay, O, lse, W, workspace, stream=None):
     """lse: float32 [Hq, n_q] or None; W: float32 [B, Hkv, max_pages * page] or None."""
-    _check(_on_device_of(Q, stream, lambda st: load_library().csat_cache_attention(
-        context(), ctypes.byref(dims), ctypes.byref(cache), _ptr(Q), _ptr(q_offsets), scale, decay, _ptr(O), _ptr(lse), _ptr(W), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), st)))
+    _issue("csat_cache_attention", Q, stream, (
+        ctypes.byref(dims), ctypes.byref(cache), Q.data_ptr(), q_offsets.data_ptr(), scale, decay, O.data_ptr(), _at(lse), _at(W),
+        _at(workspace), 0 if workspace is None else workspace.numel()))
 
 
 def csat_cache_evict(dims, cache, to, W, W_to, budget, recent, kept, stream=None):
     """kept: int32 [B, Hkv, budget]; to.lengths is written."""
-    _check(_on_device_of(W, stream, lambda st: load_library().csat_cache_evict(
-        context(), ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(to), _ptr(W), _ptr(W_to), budget, recent, _ptr(kept), st)))
+    _issue("csat_cache_evict", W, stream, (
+        ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(to), W.data_ptr(), W_to.data_ptr(), budget, recent, kept.data_ptr()))
 
 
 def csat_profile_enable(on: bool):

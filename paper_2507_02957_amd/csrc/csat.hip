@@ -2222,14 +2222,15 @@ CacheView cache_view(const csat_cache& c) {
     return v;
 }
 
-struct CachedPlan { int tiles, shares, score_ld; size_t part_bytes, bytes; };
-// The tokens in shares until there are four workgroups for every compute unit, a share no shorter than 512 tokens.
+struct CachedPlan { int tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; };
+// Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike.
+constexpr int kShareTokens = 512;
 CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weights) {
     CachedPlan p{};
     const long long rows = (long long)longest_q(d) * (d.Hq / d.Hkv);
     p.tiles = (int)((rows + 15) / 16);
-    const long long groups = (long long)d.B * d.Hkv * p.tiles;
-    p.shares = (int)std::max(1LL, std::min<long long>(1024 / groups, c.max_len / 512));
+    p.share_tokens = getenv("CSAT_SHARE") ? atoi(getenv("CSAT_SHARE")) : kShareTokens;
+    p.shares = (c.max_len + p.share_tokens - 1) / p.share_tokens;
     p.score_ld = (int)round_up(c.max_len, 64);
     p.part_bytes = p.shares > 1 || weights ? (size_t)round_up((long long)p.shares * d.n_q * d.Hq * (d.d + 2) * 4, 256) : 0;
     p.bytes = p.part_bytes + (weights ? (size_t)d.B * d.Hkv * rows * p.score_ld * 4 : 0);
@@ -2835,7 +2836,7 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     HIP_TRY(d.dtype == CSAT_BF16 ? prompt_launch_bf16(a, st) : prompt_launch_f32(a, st));
     if (p.shares > 1) {
         tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
-        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares};
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares, nullptr, 0, 0};
         HIP_TRY(d.dtype == CSAT_BF16 ? attention_join_launch_bf16(j, st) : attention_join_launch_f32(j, st));
     }
     return CSAT_OK;
@@ -2897,7 +2898,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     a.q_token = d.q_token; a.q_head = d.q_head; a.o_token = d.o_token; a.o_head = d.o_head;
     a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.d = d.d; a.n_q = d.n_q; a.max_q = longest_q(d); a.causal = d.causal != 0;
     a.sl = scale * 1.4426950408889634f;
-    a.tiles = p.tiles; a.shares = p.shares;
+    a.tiles = p.tiles; a.shares = p.shares; a.share_tokens = p.share_tokens;
     a.part = p.part_bytes ? (float*)workspace : nullptr;
     a.scores = W ? (float*)((char*)workspace + p.part_bytes) : nullptr;
     a.score_ld = p.score_ld; a.W = W; a.decay = decay;
@@ -2905,9 +2906,8 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     HIP_TRY(cache_attention_launch(d.dtype == CSAT_BF16, a, st));
     if (a.part) {
         tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
-        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares};
-        HIP_TRY(d.dtype == CSAT_BF16 ? attention_join_launch_bf16(j, st) : attention_join_launch_f32(j, st));
-        if (W) HIP_TRY(cache_weights_launch(a, st));
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares, cache->lengths, p.share_tokens, cache->max_len};
+        HIP_TRY(cache_join_launch(d.dtype == CSAT_BF16, j, a, st));
     }
     return CSAT_OK;
 }

@@ -177,7 +177,7 @@ struct CachedArgs {
     int B, Hq, Hkv, G, d, n_q, max_q, causal;
     float sl;                      // scale log2(e)
     int tiles;                     // 16-row tiles per sequence and key head
-    int shares;                    // workgroups that split a sequence's tokens
+    int shares, share_tokens;      // the longest sequence's shares of share_tokens (a multiple of 64); a sequence has those it needs
     float* part;                   // [shares][n_q Hq][d], then [shares][n_q Hq][2] as in csat_prompt.h, or null: O and lse are written
     float* scores;                 // [B][Hkv][max_q G][score_ld] in units of log2, for the weights, or null
     int score_ld;
@@ -207,17 +207,17 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
     const uint32_t n = nan_codes(w);
     return w & ~((n - (n >> 7)) | n);
 }
-__device__ __forceinline__ uint32_t one_where_nan(uint32_t w) { return (nan_codes(w) >> 7) * 0x38u; }      // 0x38: 1.0
 
 // A tile is 64 tokens by 16 rows.  S^T = K Q^T with 16 x 16 x 32 instructions: instruction row i of sub-tile s is token
 // 16 (i / 4) + 4 s + i % 4, so that a lane's 16 scores are those of the 16 consecutive tokens 16 quad .. + 15 of one query
 // row, and, as the B operand of O^T = V^T P^T, meet 16 consecutive bytes of V^T.  A wavefront takes every fourth tile of its
 // share and keeps a running maximum and sum of its own; the four are joined through LDS at the end.
+template <int DC> constexpr int cached_lds_bytes(int d) { return 4 * 16 * (d + 4) * 4 + 4 * 16 * 8 + 64 * DC * 4; }
 template <typename T, int DC>
-__global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
+__global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(CachedArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3;      // float queries and weights as three bf16 parts: 24 bits
     constexpr int DT = 4 * DC;
-    extern __shared__ float joint[];                // [4][16][d + 4] outputs, then [4][16][2]
+    extern __shared__ float joint[];                // [4][16][d + 4] outputs, then [4][16][2]; a token per feature, of its first NaN
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int hk = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv % a.tiles, share = blockIdx.x / a.Hkv / a.tiles % a.shares;
@@ -235,8 +235,9 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
     };
     const int r_last = r_base + 16 < rows ? r_base + 15 : rows - 1;
     const int lo = limit_of(r_base), hi = limit_of(r_last);
-    const int steps = (hi + 63) / 64;
-    const int t0 = (int)((long long)steps * share / a.shares), t1 = (int)((long long)steps * (share + 1) / a.shares);
+    const int s0 = share * a.share_tokens, s1 = s0 + a.share_tokens < hi ? s0 + a.share_tokens : hi;
+    if (s0 >= L && share > 0) return;
+    const int t0 = s0 / 64, t1 = (s1 + 63) / 64;     // (none where no row of the tile sees the share)
     const int r = r_base + li < rows ? r_base + li : rows - 1;
     const int tok = r / a.G, head = hk * a.G + r % a.G, lim = limit_of(r);
 
@@ -264,6 +265,11 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
                 }
             }
     }
+    const int pitch = a.d + 4;
+    float2* const ml = (float2*)(joint + 4 * 16 * pitch);
+    int* const nan_at = (int*)(ml + 4 * 16);
+    for (int i = tid; i < 64 * DC; i += 256) nan_at[i] = kNoKey;
+    __syncthreads();
     f32x4 o[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -279,20 +285,39 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
         if (id < 0 || id >= a.c.pages) { bad = true; id = 0; }
         return id;
     };
-    for (int t = t0 + wave; t < t1; t += 4) {
-        const int first = 64 * t;
-        const int kt = first + 16 * (li >> 2), vt = first + 16 * quad;
-        const int kid = page_of(kt), vid = page_of(vt);
+    // A step's loads are issued as soon as the registers of the step before are free (K behind its products, V behind its own), the
+    // pages they need are looked up another step ahead: memory is never waited for from a standstill.
+    uint4 kw[4][DC], vw[DT];
+    float kscale, vscale;
+    auto load_k = [&](int t, int kid, int vid) {
+        const int kt = 64 * t + 16 * (li >> 2);
         const uint8_t* kp = a.c.K + ((long long)kid * a.Hkv + hk) * head_bytes + (long long)((kt & (page - 1)) + (li & 3)) * a.d + 16 * quad;
-        const uint8_t* vp = a.c.V + ((long long)vid * a.Hkv + hk) * head_bytes + (long long)li * page + (vt & (page - 1));
-        const float kscale = a.c.Ks[(long long)vid * a.Hkv + hk] * a.sl, vscale = a.c.Vs[(long long)vid * a.Hkv + hk];
-        uint4 kw[4][DC], vw[DT];
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int c = 0; c < DC; ++c) kw[s][c] = 64 * c + 16 * quad < a.d ? *(const uint4*)(kp + (long long)(4 * s) * a.d + 64 * c) : uint4{0u, 0u, 0u, 0u};
+        kscale = a.c.Ks[(long long)vid * a.Hkv + hk] * a.sl;
+    };
+    auto load_v = [&](int t, int vid) {
+        const int vt = 64 * t + 16 * quad;
+        const uint8_t* vp = a.c.V + ((long long)vid * a.Hkv + hk) * head_bytes + (long long)li * page + (vt & (page - 1));
 #pragma unroll
         for (int u = 0; u < DT; ++u) vw[u] = 16 * u < a.d ? *(const uint4*)(vp + (long long)(16 * u) * page) : uint4{0u, 0u, 0u, 0u};
+        vscale = a.c.Vs[(long long)vid * a.Hkv + hk];
+    };
+    int kid = 0, vid = 0, kid2 = 0, vid2 = 0;        // of the next step, of the one behind it
+    if (t0 + wave < t1) {
+        const int t = t0 + wave;
+        kid = page_of(64 * t + 16 * (li >> 2));
+        vid = page_of(64 * t + 16 * quad);
+        if (t + 4 < t1) { kid2 = page_of(64 * (t + 4) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 4) + 16 * quad); }
+        load_k(t, kid, vid);
+        load_v(t, vid);
+        kid = kid2; vid = vid2;
+    }
+    for (int t = t0 + wave; t < t1; t += 4) {
+        const int first = 64 * t, vt = first + 16 * quad;
+        if (t + 8 < t1) { kid2 = page_of(64 * (t + 8) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 8) + 16 * quad); }
 
         float e[16];
 #pragma unroll
@@ -310,6 +335,9 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) e[4 * s + i] = acc[i] * kscale;
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 4 < t1) load_k(t + 4, kid, vid);
+        __builtin_amdgcn_sched_barrier(0);
         const bool masks = first + 64 > lo;
         if (masks) {
 #pragma unroll
@@ -353,29 +381,23 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
                     x -= (float)pf[p][h][i];
                 }
             }
-        bool odd = false;
-        if (masks) {
+        if (masks) {      // NaN codes out of tokens that some row does not see (0 times NaN is NaN), the first of each feature noted
             uint32_t any = 0;
 #pragma unroll
             for (int u = 0; u < DT; ++u) any |= nan_codes(vw[u].x) | nan_codes(vw[u].y) | nan_codes(vw[u].z) | nan_codes(vw[u].w);
-            odd = __builtin_amdgcn_ballot_w64(any != 0) != 0;
-        }
-        if (odd) {      // a NaN reaches the rows that see its token: the others have weight 0 for it, and 0 times NaN is NaN
-            bf16x8 ones[2];
+            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int u = 0; u < DT; ++u) {
+                    int at = 16;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ones[h][i] = vt + 8 * h + i < lim ? (__bf16)1.f : (__bf16)0.f;
-#pragma unroll
-            for (int u = 0; u < DT; ++u) {
-                f32x4 cnt = f32x4{0.f, 0.f, 0.f, 0.f};
-                const uint4 w = vw[u];
-                cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(code_fragment(one_where_nan(w.x), one_where_nan(w.y)), ones[0], cnt, 0, 0, 0);
-                cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(code_fragment(one_where_nan(w.z), one_where_nan(w.w)), ones[1], cnt, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (cnt[i] > 0.f) o[u][i] = __uint_as_float(0x7fc00000u);
-                vw[u] = uint4{without_nan(w.x), without_nan(w.y), without_nan(w.z), without_nan(w.w)};
+                    for (int i = 3; i >= 0; --i) {
+                        uint32_t& w = (&vw[u].x)[i];
+                        const uint32_t n = nan_codes(w);
+                        if (n) at = 4 * i + (__ffs(n) - 1) / 8;
+                        w = without_nan(w);
+                    }
+                    if (at < 16) atomicMin(nan_at + 16 * u + li, vt + at);
+                }
             }
         }
 #pragma unroll
@@ -387,11 +409,12 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
                 o[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[p][1], o[u], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 4 < t1) load_v(t + 4, vid);
+        kid = kid2; vid = vid2;
     }
 
     // the wavefronts' parts of a row, brought to the largest reference
-    const int pitch = a.d + 4;
-    float2* const ml = (float2*)(joint + 4 * 16 * pitch);
     sum = quad_sum(sum);
     if (__builtin_amdgcn_ballot_w64(bad) != 0) sum = __uint_as_float(0x7fc00000u);
 #pragma unroll
@@ -414,7 +437,10 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
             total += k * y.y;
             x[0] += k * z.x; x[1] += k * z.y; x[2] += k * z.z; x[3] += k * z.w;
         }
-        const int rr = r_base + i, h = hk * a.G + rr % a.G;
+        const int rr = r_base + i, h = hk * a.G + rr % a.G, seen = limit_of(rr);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (nan_at[f + e] < seen) x[e] = __uint_as_float(0x7fc00000u);
         const long long row = qs.first + rr / a.G;
         if (a.part) {
             const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + h;
@@ -430,39 +456,53 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(CachedArgs a) {
     }
 }
 
-// W = decay W + sum over rows of 2^(score - lse), a thread four tokens.
-static __global__ __launch_bounds__(256) void cache_weights_kernel(CachedArgs a) {
+// The second launch: the first o_blocks workgroups join a row of O each, the others form W = decay W + sum over rows of
+// 2^(score - lse) for 1024 tokens of a sequence and key head, a thread four of them.
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs a, int o_blocks) {
     constexpr int RB = 64;
     __shared__ float lse2[RB];
     __shared__ int limit[RB];
-    const int tid = threadIdx.x;
-    const int chunks = (a.c.max_len + 1023) / 1024;
-    const int chunk = blockIdx.x % chunks, hk = blockIdx.x / chunks % a.Hkv, b = blockIdx.x / chunks / a.Hkv;
+    if ((int)blockIdx.x < o_blocks) {
+        const int per = j.max_q * j.Hq;
+        join_row<T>(j, blockIdx.x / per, blockIdx.x % per);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int chunks = (a.c.max_len + 1023) / 1024, id = blockIdx.x - o_blocks;
+    const int chunk = id % chunks, hk = id / chunks % a.Hkv, b = id / chunks / a.Hkv;
     const int L = a.c.lengths[b], t = chunk * 1024 + 4 * tid;
     if (L < 0 || L > a.c.max_len || chunk * 1024 >= L) return;
     const PackedSpan qs(a.q_off, b, a.n_q);
     const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G;
     const long long all = (long long)a.n_q * a.Hq;
     const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d);
+    const int shares = shares_of(a.c.lengths, b, a.share_tokens, a.c.max_len, a.shares);
     float* const w = a.W + ((long long)b * a.Hkv + hk) * a.c.max_pages * a.c.page + t;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < rows; r0 += RB) {
+        const int n = rows - r0 < RB ? rows - r0 : RB;
         __syncthreads();
-        if (tid < RB && r0 + tid < rows) {
-            const int r = r0 + tid;
+        for (int i = tid >> 6; i < n; i += 4) {      // a wavefront a row
+            const int r = r0 + i;
             const long long at = (long long)(qs.first + r / a.G) * a.Hq + hk * a.G + r % a.G;
             float off = INFINITY, total = 0.f;
-            for (int s = 0; s < a.shares; ++s) off = fminf(off, ml[(long long)s * all + at].x);
-            for (int s = 0; s < a.shares; ++s) {
+            for (int s = lane; s < shares; s += 64) off = fminf(off, ml[(long long)s * all + at].x);
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) off = fminf(off, __shfl_xor(off, s));
+            for (int s = lane; s < shares; s += 64) {
                 const float2 y = ml[(long long)s * all + at];
                 if (y.x != INFINITY) total += __builtin_amdgcn_exp2f(off - y.x) * y.y;
             }
-            lse2[tid] = total == 0.f ? INFINITY : __log2f(total) - off;      // (nothing seen: weights 0)
-            int v = a.causal ? r / a.G + L - qs.count + 1 : L;
-            limit[tid] = v < 0 ? 0 : v > L ? L : v;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
+            const int v = a.causal ? r / a.G + L - qs.count + 1 : L;
+            if (lane == 0) {
+                lse2[i] = total == 0.f ? INFINITY : __log2f(total) - off;      // (nothing seen: weights 0)
+                limit[i] = v < 0 ? 0 : v > L ? L : v;
+            }
         }
         __syncthreads();
-        const int n = rows - r0 < RB ? rows - r0 : RB;
         if (t >= L) continue;
         const float* s = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G + r0) * a.score_ld + t;
         for (int i = 0; i < n; ++i, s += a.score_ld) {

@@ -70,7 +70,7 @@ hipError_t attention_join_launch_f32(const JoinArgs& a, hipStream_t st);
 // The 8-bit cache (csat_cache.h).  blocks: the most that a sequence and head has after an eviction.
 hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st);
 hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st);
-hipError_t cache_weights_launch(const CachedArgs& a, hipStream_t st);
+hipError_t cache_join_launch(bool bf16, const JoinArgs& j, const CachedArgs& a, hipStream_t st);
 hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st);
 
 }  // namespace csat

@@ -387,8 +387,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
     }
 }
 
-// Shares of a row's keys -> the row: offsets brought to the smallest, outputs and sums added in the order of the shares.
-// One wavefront per row.
+// Shares of a row's keys -> the row: offsets brought to the smallest, outputs and sums added, a workgroup's wavefronts every fourth
+// share each and then in order.  One workgroup per row.
 struct JoinArgs {
     const float* part;             // [shares][n_q Hq][d], then [shares][n_q Hq][2]: offset (+inf: nothing seen), sum
     void* O;
@@ -396,41 +396,80 @@ struct JoinArgs {
     const int* q_off;
     long long o_token, o_head;
     int B, Hq, Hkv, G, d, n_q, max_q, shares;
+    const int* lengths;            // the sequences' keys, where a share is `share_keys` of them and a sequence has only those it needs; or null
+    int share_keys, max_len;
 };
+__device__ __forceinline__ int shares_of(const int* lengths, int b, int share_keys, int max_len, int shares) {
+    if (!lengths) return shares;
+    const int L = lengths[b];
+    return L <= 0 || L > max_len ? 1 : (L + share_keys - 1) / share_keys;
+}
 
+constexpr int kJoinAhead = 8;      // shares whose outputs a wavefront has in flight
 template <typename T>
-__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int per = (a.max_q * a.Hq + 3) / 4;
-    const int b = blockIdx.x / per, r = (blockIdx.x % per) * 4 + (threadIdx.x >> 6);
+__device__ __forceinline__ void join_row(const JoinArgs& a, int b, int r) {
+    __shared__ float4 outs[4][64];
+    __shared__ float sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const PackedSpan qs(a.q_off, b, a.n_q);
     const int tok = r / a.Hq, head = r % a.Hq;
     if (tok >= (qs.count < a.max_q ? qs.count : a.max_q)) return;
+    const int shares = shares_of(a.lengths, b, a.share_keys, a.max_len, a.shares);
     const long long row = qs.first + tok, all = (long long)a.n_q * a.Hq, at = row * a.Hq + head;
     const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d) + at;
-    float off = INFINITY, bad = 0.f;
-    for (int s = 0; s < a.shares; ++s) {
+    float off = INFINITY, odd = 0.f;
+    for (int s = lane; s < shares; s += 64) {
         const float x = ml[(long long)s * all].x;
         off = fminf(off, x);
-        if (x != x) bad = x;
+        if (x != x) odd = x;
     }
-    float total = bad, o[4] = {bad, bad, bad, bad};      // columns 4 lane .. + 3
-    for (int s = 0; s < a.shares; ++s) {
-        const float2 x = ml[(long long)s * all];
-        if (x.x == INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(off - x.x);
-        total += f * x.y;
-        if (4 * lane < a.d) {
-            const float4 p = *(const float4*)(a.part + ((long long)s * all + at) * a.d + 4 * lane);
-            o[0] += f * p.x; o[1] += f * p.y; o[2] += f * p.z; o[3] += f * p.w;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        off = fminf(off, __shfl_xor(off, s));
+        odd += __shfl_xor(odd, s);                   // (0, or NaN)
+    }
+    const bool cols = 4 * lane < a.d;
+    const float* const p = a.part + at * a.d + 4 * lane;
+    float total = odd;
+    float4 o = float4{odd, odd, odd, odd};           // columns 4 lane .. + 3
+    for (int s0 = wave; s0 < shares; s0 += 4 * kJoinAhead) {
+        float4 x[kJoinAhead];
+        float2 y[kJoinAhead];
+#pragma unroll
+        for (int i = 0; i < kJoinAhead; ++i) {
+            const int s = s0 + 4 * i;
+            y[i] = s < shares ? ml[(long long)s * all] : float2{INFINITY, 0.f};
+            x[i] = s < shares && cols ? *(const float4*)(p + (long long)s * all * a.d) : float4{0.f, 0.f, 0.f, 0.f};
         }
+#pragma unroll
+        for (int i = 0; i < kJoinAhead; ++i) {
+            if (y[i].x == INFINITY) continue;
+            const float f = __builtin_amdgcn_exp2f(off - y[i].x);
+            total += f * y[i].y;
+            o.x += f * x[i].x; o.y += f * x[i].y; o.z += f * x[i].z; o.w += f * x[i].w;
+        }
+    }
+    outs[wave][lane] = o;
+    if (lane == 0) sums[wave] = total;
+    __syncthreads();
+    if (wave != 0) return;
+    total = sums[0] + sums[1] + sums[2] + sums[3];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float4 x = outs[w][lane];
+        o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
     if (a.lse && lane == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off);
-    if (4 * lane >= a.d) return;
+    if (!cols) return;
     T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head + 4 * lane;
-    if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(o[0] * inv, o[1] * inv), f2bf_pk(o[2] * inv, o[3] * inv)};
-    else *(float4*)out = float4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+    if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(o.x * inv, o.y * inv), f2bf_pk(o.z * inv, o.w * inv)};
+    else *(float4*)out = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
+}
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) {
+    const int per = a.max_q * a.Hq;
+    join_row<T>(a, blockIdx.x / per, blockIdx.x % per);
 }
 
 }  // namespace csat

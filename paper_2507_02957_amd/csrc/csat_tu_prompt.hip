@@ -18,8 +18,10 @@ typedef float T;
 
 hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, hipStream_t st) {
     auto launch = [&](auto kernel, int lds_bytes) -> hipError_t {
-        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-        if (e != hipSuccess) return e;
+        if (lds_bytes > 64 * 1024) {
+            const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+            if (e != hipSuccess) return e;
+        }
         hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.B * a.Hkv * a.tiles * a.shares)), dim3(64 * kPromptWaves), lds_bytes, st, a);
         return hipGetLastError();
     };
@@ -32,7 +34,7 @@ hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, hipStream_t st) {
 }
 
 hipError_t CSAT_TU_FN(attention_join_launch)(const JoinArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)(a.B * (((long long)a.max_q * a.Hq + 3) / 4))), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((long long)a.B * a.max_q * a.Hq)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

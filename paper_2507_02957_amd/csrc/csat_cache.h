@@ -63,11 +63,32 @@ __device__ __forceinline__ float wave_max(float x) {
     return x;
 }
 
-// One workgroup per touched block (K and V of it).  Two passes over its new rows, the second of which finds them in the
-// cache: the largest finite magnitudes, then the codes.
-template <typename T>
+// 4 x 4 bytes: word i's byte j becomes word j's byte i
+__device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
+    const uint32_t a0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), a1 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);      // w0 w1 bytes 0, 1 in turn
+    const uint32_t b0 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), b1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(a1, a0, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(b1, b0, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+}
+// bytes of a word at slot s that lie in [lo, hi)
+__device__ __forceinline__ uint32_t byte_mask(int s, int lo, int hi) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m |= s + e >= lo && s + e < hi ? 0xffu << (8 * e) : 0u;
+    return m;
+}
+
+// One workgroup per touched block (K and V of it).  A thread holds NI pieces of 4 tokens by 4 features of both, so memory is read
+// once: largest finite magnitudes over the workgroup, the codes, K's rows straight to memory, V's 4 x 4 bytes turned and
+// through LDS, from which they leave 16 tokens of a feature at a time, next to what older tokens the 16 hold.
+// Bound by memory: (2 or 4) + 1 bytes a value in and out.
+constexpr int store_lds_bytes(int d, int page) { return d * (page + 4); }
+template <typename T, int NI>
 __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     __shared__ float red[2][4];
+    extern __shared__ uint4 turned[];                // [d][page + 4] codes of V
     const int tid = threadIdx.x;
     const int hk = blockIdx.x % a.Hkv, i = blockIdx.x / a.Hkv % a.reach, b = blockIdx.x / a.Hkv / a.reach;
     const PackedSpan ks(a.k_off, b, a.n_k);
@@ -77,91 +98,106 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     const int start = len - n, page = a.c.page, first = start >> a.c.log_page, last = (len - 1) >> a.c.log_page;
     const int j = first + i;
     if (j > last) return;
-    // a sequence with a page that does not exist is not stored to at all
-    bool bad = false;
-    for (int t = first + tid; t <= last; t += 256) {
-        const int p = a.c.table[(long long)b * a.c.max_pages + t];
-        bad |= p < 0 || p >= a.c.pages;
-    }
-    if (__syncthreads_or(bad)) return;
-    const int id = a.c.table[(long long)b * a.c.max_pages + j];
+    const int* const table = a.c.table + (long long)b * a.c.max_pages;
     const int lo = j == first ? start - j * page : 0, hi = j == last ? len - j * page : page;      // new slots
     const long long row0 = ks.first + ((long long)j * page - start);      // packed row of slot 0
     const T* K = (const T*)a.K + row0 * a.k_token + (long long)hk * a.k_head;
     const T* V = (const T*)a.V + row0 * a.v_token + (long long)hk * a.v_head;
-    const long long block = (long long)id * a.Hkv + hk;
-    uint8_t* const ck = a.c.K + block * page * a.d;
-    uint8_t* const cv = a.c.V + block * page * a.d;
-
-    const int dq = a.d / 4;                 // pieces of four features
-    float mk = 0.f, mv = 0.f;
-    auto four = [](const T* p, float* x) {
+    const int dq = a.d / 4, items = page / 4 * dq;
+    typedef typename std::conditional<sizeof(T) == 2, uint2, float4>::type Four;
+    Four xk[NI][4], xv[NI][4];
+    bool bad = false;
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, s = q / dq * 4, f = q % dq * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            xk[p][e] = xv[p][e] = Four{};
+            if (q < items && s + e >= lo && s + e < hi) {
+                xk[p][e] = *(const Four*)(K + (long long)(s + e) * a.k_token + f);
+                xv[p][e] = *(const Four*)(V + (long long)(s + e) * a.v_token + f);
+            }
+        }
+    }
+    // a sequence with a page that does not exist is not stored to at all
+    for (int t = first + tid; t <= last; t += 256) bad |= table[t] < 0 || table[t] >= a.c.pages;
+    auto four = [](const Four& w, float* x) {
         if constexpr (sizeof(T) == 2) {
-            const uint2 w = *(const uint2*)p;
             x[0] = __uint_as_float(w.x << 16); x[1] = __uint_as_float(w.x & 0xffff0000u);
             x[2] = __uint_as_float(w.y << 16); x[3] = __uint_as_float(w.y & 0xffff0000u);
         } else {
-            const float4 w = *(const float4*)p;
             x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w;
         }
     };
-    for (int q = tid; q < (hi - lo) * dq; q += 256) {
-        const int s = lo + q / dq, f = q % dq * 4;
-        float x[4];
-        four(K + (long long)s * a.k_token + f, x);
-        mk = fmaxf(mk, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
-        four(V + (long long)s * a.v_token + f, x);
-        mv = fmaxf(mv, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
-    }
+    float mk = 0.f, mv = 0.f;
+#pragma unroll
+    for (int p = 0; p < NI; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x[4];
+            four(xk[p][e], x);
+            mk = fmaxf(mk, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
+            four(xv[p][e], x);
+            mv = fmaxf(mv, fmaxf(fmaxf(finite_abs(x[0]), finite_abs(x[1])), fmaxf(finite_abs(x[2]), finite_abs(x[3]))));
+        }
     mk = wave_max(mk);
     mv = wave_max(mv);
     if ((tid & 63) == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
+    if (__syncthreads_or(bad)) return;
+    const long long block = (long long)table[j] * a.Hkv + hk;
     const float ok = lo ? a.c.Ks[block] : 0.f, ov = lo ? a.c.Vs[block] : 0.f;
-    __syncthreads();
+    uint8_t* const ck = a.c.K + block * page * a.d;
+    uint8_t* const cv = a.c.V + block * page * a.d;
     mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
     mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
     const float sk = fmaxf(pow2f(scale_exponent(mk)), ok), sv = fmaxf(pow2f(scale_exponent(mv)), ov);
-    if (tid == 0) { a.c.Ks[block] = sk; a.c.Vs[block] = sv; }
     const float ik = pow2f(-exponent_of(sk)), iv = pow2f(-exponent_of(sv));
 
-    for (int q = tid; q < (hi - lo) * dq; q += 256) {
-        const int s = lo + q / dq, f = q % dq * 4;
-        float x[4];
-        four(K + (long long)s * a.k_token + f, x);
-        *(uint32_t*)(ck + (long long)s * a.d + f) = to_codes(x[0] * ik, x[1] * ik, x[2] * ik, x[3] * ik);
+    const int pitch = page + 4;
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, s = q / dq * 4, f = q % dq * 4;
+        if (q >= items || s + 4 <= lo || s >= hi) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x[4];
+            four(xk[p][e], x);
+            if (s + e >= lo && s + e < hi) *(uint32_t*)(ck + (long long)(s + e) * a.d + f) = to_codes(x[0] * ik, x[1] * ik, x[2] * ik, x[3] * ik);
+            four(xv[p][e], x);
+            w[e] = to_codes(x[0] * iv, x[1] * iv, x[2] * iv, x[3] * iv);
+        }
+        transpose_bytes(w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *(uint32_t*)((uint8_t*)turned + (f + e) * pitch + s) = w[e];
     }
     if (lo && sk != ok) {
         const float f = ok * ik;
         for (int q = tid; q < lo * dq; q += 256) ((uint32_t*)ck)[q] = rescale_codes(((uint32_t*)ck)[q], f);
     }
-    // V: a thread takes one feature of sixteen tokens
+    __syncthreads();
+    if (tid == 0) { a.c.Ks[block] = sk; a.c.Vs[block] = sv; }      // (behind the barrier: every thread has read the old ones)
     const int groups = page / 16;
+    const float fv = ov * iv;
     for (int q = tid; q < groups * a.d; q += 256) {
-        const int f = q % a.d, g = q / a.d * 16;
+        const int g = q % groups * 16, f = q / groups;
         if (g >= hi || (g + 16 <= lo && sv == ov)) continue;
-        uint8_t* const out = cv + (long long)f * page + g;
-        uint4 w = uint4{0u, 0u, 0u, 0u};
-        const bool whole = g >= lo && g + 16 <= hi;
-        if (!whole) w = *(const uint4*)out;
+        uint4* const out = (uint4*)(cv + (long long)f * page + g);
+        uint4 w;
 #pragma unroll
-        for (int k = 0; k < 16; k += 4) {
-            float x[4];
-            uint32_t keep = 0;      // bytes of this word that are old or behind the new ones
-            const uint32_t was = (&w.x)[k / 4];
-            uint32_t old = was;
-            if (sv != ov && g + k < lo) old = rescale_codes(was, ov * iv);
-            uint32_t mix = 0;
+        for (int k = 0; k < 4; ++k) (&w.x)[k] = *(const uint32_t*)((const uint8_t*)turned + f * pitch + g + 4 * k);
+        if (g < lo || g + 16 > hi) {
+            const uint4 was = *out;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int s = g + k + e;
-                x[e] = 0.f;
-                if (s < lo) { keep |= 0xffu << (8 * e); mix |= old & (0xffu << (8 * e)); }
-                else if (s >= hi) { keep |= 0xffu << (8 * e); mix |= was & (0xffu << (8 * e)); }
-                else x[e] = Elem<T>::load(V + (long long)s * a.v_token + f) * iv;
+            for (int k = 0; k < 4; ++k) {
+                const int s = g + 4 * k;
+                const uint32_t in = byte_mask(s, lo, hi), old = byte_mask(s, 0, lo);
+                uint32_t x = (&was.x)[k];
+                if (old && sv != ov) x = (rescale_codes(x, fv) & old) | (x & ~old);
+                (&w.x)[k] = ((&w.x)[k] & in) | (x & ~in);
             }
-            (&w.x)[k / 4] = (to_codes(x[0], x[1], x[2], x[3]) & ~keep) | mix;
         }
-        *(uint4*)out = w;
+        *out = w;
     }
 }
 
@@ -647,78 +683,147 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
 }
 
 // One workgroup per destination block: gathers its tokens' codes of K and V, each under its source's scale, and rounds them to
-// the block's own.
-static __global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a, int blocks) {
+// the block's own.  K's rows come straight into registers.  V's tokens lie a byte each in lines that hold a page's other tokens
+// too, so the source pages pass through LDS whole, as many at a time as gather_pages() says, and a thread picks 16 tokens of
+// a feature from there; both are held until the block's scale is known.  Bound by memory: what is kept once in and once
+// out, and the rest of V's source pages.
+constexpr int kGatherLds = 36 * 1024;
+constexpr int gather_page_bytes(int d, int page) { return d * (page + 4); }
+constexpr int gather_pages(int d, int page) {
+    const int n = kGatherLds / gather_page_bytes(d, page);
+    return n < 1 ? 1 : n > 8 ? 8 : n;
+}
+__device__ __forceinline__ float largest_code(uint32_t w) {      // (the maximum passes over NaN)
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return fmaxf(fmaxf(fabsf(lo[0]), fabsf(lo[1])), fmaxf(fabsf(hi[0]), fabsf(hi[1])));
+}
+template <int NI>      // 16-byte pieces of K, and of V, per thread
+__global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a, int blocks) {
+    extern __shared__ uint4 staged[];
     __shared__ long long src_block[128];      // page * Hkv + head
-    __shared__ int src_slot[128];
+    __shared__ int src_slot[128], src_page[128];      // slot in the source page; which of the different source pages it is
+    __shared__ int page_at[128 + 1];          // first token of each different source page
     __shared__ float src_k[128], src_v[128];
     __shared__ float red[2][4];
-    const int tid = threadIdx.x, page = a.from.page, d = a.d;
+    __shared__ int different;
+    const int tid = threadIdx.x, lane = tid & 63, page = a.from.page, d = a.d;
     const int hk = blockIdx.x % a.Hkv, j = blockIdx.x / a.Hkv % blocks, b = blockIdx.x / a.Hkv / blocks;
     const int keep = a.to.lengths[b];
     if (j * page >= keep) return;             // (-1: nothing)
     const int n = keep - j * page < page ? keep - j * page : page;
     const int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget + (long long)j * page;
-    for (int i = tid; i < n; i += 256) {
-        const int t = kept[i];
-        const long long block = (long long)a.from.table[(long long)b * a.from.max_pages + (t >> a.from.log_page)] * a.Hkv + hk;
-        src_block[i] = block;
-        src_slot[i] = t & (page - 1);
-        src_k[i] = a.from.Ks[block];
-        src_v[i] = a.from.Vs[block];
-    }
-    __syncthreads();
     const long long size = (long long)page * d, dst = (long long)a.to.table[(long long)b * a.to.max_pages + j] * a.Hkv + hk;
-    // magnitudes: a code's low seven bits are in the order of the values, NaN (0x7f) above all
-    auto largest = [](uint32_t w) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t c = (w >> (8 * e)) & 0x7fu;
-            m = c != 0x7fu && c > m ? c : m;
+    {
+        int p = -1;
+        if (tid < n) {
+            const int t = kept[tid];
+            p = t >> a.from.log_page;
+            const long long block = (long long)a.from.table[(long long)b * a.from.max_pages + p] * a.Hkv + hk;
+            src_block[tid] = block;
+            src_slot[tid] = t & (page - 1);
+            src_k[tid] = a.from.Ks[block];
+            src_v[tid] = a.from.Vs[block];
         }
-        return m;
-    };
-    auto value = [](uint32_t c) { return (float)__builtin_amdgcn_cvt_pk_f32_fp8((int)c, false)[0]; };
-    const int dq = d / 4, groups = (n + 3) / 4;
-    float mk = 0.f, mv = 0.f;
-    for (int q = tid; q < n * dq; q += 256) {
-        const int i = q / dq, f = q % dq * 4;
-        mk = fmaxf(mk, value(largest(*(const uint32_t*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f))) * src_k[i]);
+        // tokens are in slot order: a new page begins where its number differs from the one before
+        const int before = tid < n && tid > 0 ? kept[tid - 1] >> a.from.log_page : -1;
+        const unsigned long long starts = __ballot(tid < n && p != before);
+        __shared__ int in_first;
+        if (tid == 0) in_first = __popcll(starts);
+        __syncthreads();
+        if (tid < n) {
+            const int u = __popcll(starts & (lane == 63 ? ~0ull : (2ull << lane) - 1ull)) - 1 + (tid >= 64 ? in_first : 0);
+            src_page[tid] = u;
+            if (p != before) page_at[u] = tid;
+            if (tid == n - 1) { different = u + 1; page_at[u + 1] = n; }
+        }
+        __syncthreads();
     }
-    for (int q = tid; q < d * n; q += 256) {
-        const int i = q % n, f = q / n;
-        mv = fmaxf(mv, value(largest(a.from.V[src_block[i] * size + (long long)f * page + src_slot[i]])) * src_v[i]);
+    const int dp = d / 16, groups = page / 16;
+    uint4 k[NI], v[NI];
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, i = q / dp, f = q % dp * 16;
+        k[p] = i < n ? *(const uint4*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f) : uint4{0u, 0u, 0u, 0u};
+        v[p] = uint4{0u, 0u, 0u, 0u};
+    }
+    const int pitch = page + 4, at_once = gather_pages(d, page), pieces = d * groups;
+    for (int u0 = 0; u0 < different; u0 += at_once) {
+        const int u1 = u0 + at_once < different ? u0 + at_once : different;
+        if (u0) __syncthreads();
+        for (int q = tid; q < (u1 - u0) * pieces; q += 256) {
+            const int u = q / pieces, r = q % pieces, g = r % groups * 16, f = r / groups;
+            const uint4 w = *(const uint4*)(a.from.V + src_block[page_at[u0 + u]] * size + (long long)f * page + g);
+            uint32_t* const to = (uint32_t*)((uint8_t*)staged + u * gather_page_bytes(d, page) + f * pitch + g);
+            to[0] = w.x; to[1] = w.y; to[2] = w.z; to[3] = w.w;
+        }
+        __syncthreads();
+        const int i0 = page_at[u0], i1 = page_at[u1];
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+            const int q = p * 256 + tid, f = q % d, g = q / d * 16;
+            if (g >= page || g >= i1 || g + 16 <= i0) continue;
+            const uint8_t* const src = (const uint8_t*)staged + f * pitch;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = g + e;
+                if (i >= i0 && i < i1) (&v[p].x)[e / 4] |= (uint32_t)src[(src_page[i] - u0) * gather_page_bytes(d, page) + src_slot[i]] << (8 * (e & 3));
+            }
+        }
+    }
+    float mk = 0.f, mv = 0.f;
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, i = q / dp, g = q / d * 16;
+        if (i < n) mk = fmaxf(mk, src_k[i] * fmaxf(fmaxf(largest_code(k[p].x), largest_code(k[p].y)), fmaxf(largest_code(k[p].z), largest_code(k[p].w))));
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (g + e < n) {
+                const uint32_t c = ((&v[p].x)[e / 4] >> (8 * (e & 3))) & 0xffu;
+                mv = fmaxf(mv, src_v[g + e] * fabsf(__builtin_amdgcn_cvt_pk_f32_fp8((int)c, false)[0]));
+            }
     }
     mk = wave_max(mk);
     mv = wave_max(mv);
-    if ((tid & 63) == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
+    if (lane == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
     __syncthreads();
     mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
     mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
     const int ek = scale_exponent(mk), ev = scale_exponent(mv);
     if (tid == 0) { a.to.Ks[dst] = pow2f(ek); a.to.Vs[dst] = pow2f(ev); }
     const float ik = pow2f(-ek), iv = pow2f(-ev);
-    for (int q = tid; q < n * dq; q += 256) {
-        const int i = q / dq, f = q % dq * 4;
-        const uint32_t w = *(const uint32_t*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f);
-        const float s = src_k[i] * ik;
-        *(uint32_t*)(a.to.K + dst * size + (long long)i * d + f) = s == 1.f ? w : rescale_codes(w, s);
-    }
-    for (int q = tid; q < d * groups; q += 256) {
-        const int g = q % groups * 4, f = q / groups;
-        uint32_t w = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int i = g + e < n ? g + e : n - 1;
-            const uint32_t c = a.from.V[src_block[i] * size + (long long)f * page + src_slot[i]];
-            const float s = src_v[i] * iv;
-            w |= (s == 1.f ? c : rescale_codes(c, s) & 0xffu) << (8 * e);
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, i = q / dp;
+        if (i < n) {
+            const float s = src_k[i] * ik;
+            uint4 w = k[p];
+            if (s != 1.f) w = uint4{rescale_codes(w.x, s), rescale_codes(w.y, s), rescale_codes(w.z, s), rescale_codes(w.w, s)};
+            *(uint4*)(a.to.K + dst * size + (long long)i * d + q % dp * 16) = w;
+        }
+        const int f = q % d, g = q / d * 16;
+        if (g >= n) continue;
+        uint4 w = v[p];
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            uint32_t& x = (&w.x)[e / 4];
+            float s[4];
+            bool same = true;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                s[h] = src_v[g + e + h < n ? g + e + h : n - 1] * iv;
+                same &= s[h] == 1.f;
+            }
+            if (same) continue;
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+            x = to_codes(lo[0] * s[0], lo[1] * s[1], hi[0] * s[2], hi[1] * s[3]);
         }
         uint8_t* const out = a.to.V + dst * size + (long long)f * page + g;
-        if (g + 4 <= n) *(uint32_t*)out = w;
-        else
-            for (int e = 0; g + e < n; ++e) out[e] = (uint8_t)(w >> (8 * e));
+        if (g + 16 <= n) *(uint4*)out = w;
+        else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (g + e < n) out[e] = (uint8_t)((&w.x)[e / 4] >> (8 * (e & 3)));
+        }
     }
 }
 

@@ -4,23 +4,28 @@
 
 namespace csat {
 
-hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)((long long)a.B * a.reach * a.Hkv));
-    if (bf16) hipLaunchKernelGGL(cache_store_kernel<bf16_t>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(cache_store_kernel<float>, grid, dim3(256), 0, st, a);
+template <typename K, typename... A>
+static hipError_t launch(K kernel, long long grid, int threads, int lds_bytes, hipStream_t st, A... args) {
+    if (lds_bytes > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds_bytes, st, args...);
     return hipGetLastError();
 }
 
+hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st) {
+    const int items = (a.d * a.c.page / 16 + 255) / 256;
+#define CSAT_STORE(NI_) (bf16 ? launch(cache_store_kernel<bf16_t, NI_>, (long long)a.B * a.reach * a.Hkv, 256, store_lds_bytes(a.d, a.c.page), st, a) \
+                              : launch(cache_store_kernel<float, NI_>, (long long)a.B * a.reach * a.Hkv, 256, store_lds_bytes(a.d, a.c.page), st, a))
+    return items <= 1 ? CSAT_STORE(1) : items <= 2 ? CSAT_STORE(2) : items <= 4 ? CSAT_STORE(4) : CSAT_STORE(8);
+#undef CSAT_STORE
+}
+
 hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st) {
-    auto launch = [&](auto kernel, int lds_bytes) -> hipError_t {
-        if (lds_bytes > 64 * 1024) {
-            const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-            if (e != hipSuccess) return e;
-        }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.B * a.shares * a.tiles * a.Hkv)), dim3(256), lds_bytes, st, a);
-        return hipGetLastError();
-    };
-#define CSAT_CACHED(DC_) (bf16 ? launch(cache_attention_kernel<bf16_t, DC_>, cached_lds_bytes<DC_>(a.d)) : launch(cache_attention_kernel<float, DC_>, cached_lds_bytes<DC_>(a.d)))
+    const long long grid = (long long)a.B * a.shares * a.tiles * a.Hkv;
+#define CSAT_CACHED(DC_) (bf16 ? launch(cache_attention_kernel<bf16_t, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a) \
+                               : launch(cache_attention_kernel<float, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a))
     if (a.d <= 64) return CSAT_CACHED(1);
     if (a.d <= 128) return CSAT_CACHED(2);
     return CSAT_CACHED(4);
@@ -36,11 +41,13 @@ hipError_t cache_join_launch(bool bf16, const JoinArgs& j, const CachedArgs& a, 
 }
 
 hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st) {
-    hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)(a.B * a.Hkv)), dim3(kSelectThreads), 0, st, a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch(cache_select_kernel, (long long)a.B * a.Hkv, kSelectThreads, 0, st, a);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(cache_gather_kernel, dim3((unsigned)((long long)a.B * blocks * a.Hkv)), dim3(256), 0, st, a, blocks);
-    return hipGetLastError();
+    const int items = (a.d * a.from.page / 16 + 255) / 256, lds_bytes = gather_pages(a.d, a.from.page) * gather_page_bytes(a.d, a.from.page);
+    const long long grid = (long long)a.B * blocks * a.Hkv;
+#define CSAT_GATHER(NI_) launch(cache_gather_kernel<NI_>, grid, 256, lds_bytes, st, a, blocks)
+    return items <= 1 ? CSAT_GATHER(1) : items <= 2 ? CSAT_GATHER(2) : items <= 4 ? CSAT_GATHER(4) : CSAT_GATHER(8);
+#undef CSAT_GATHER
 }
 
 }  // namespace csat

@@ -2931,7 +2931,7 @@ csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat
     EvictArgs a{};
     a.from = cache_view(*from); a.to = cache_view(*to);
     a.W = W; a.W_to = W_to; a.kept = kept;
-    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.budget = budget; a.recent = recent;
+    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.budget = budget; a.recent = recent; a.row_magic = (1 << 20) / (d.d / 16) + 1;
     Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_EVICT, st);
     HIP_TRY(cache_evict_launch(a, (most + from->page - 1) / from->page, st));
     return CSAT_OK;

@@ -36,15 +36,14 @@ __device__ __forceinline__ float finite_abs(float x) {
     return v < INFINITY ? v : 0.f;
 }
 __device__ __forceinline__ float nan_if_odd(float x) { return fabsf(x) < INFINITY ? x : __uint_as_float(0x7fc00000u); }
-// four floats (already divided by the scale) -> four codes, nearest, ties to even
-__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_odd(a), nan_if_odd(b), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(nan_if_odd(c), nan_if_odd(d), w, true);
-    return (uint32_t)w;
+// four floats (already divided by the scale) -> four codes, nearest, ties to even; codes_of: none of them infinite
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) { return codes_of(nan_if_odd(a), nan_if_odd(b), nan_if_odd(c), nan_if_odd(d)); }
 __device__ __forceinline__ uint32_t rescale_codes(uint32_t w, float f) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    return to_codes(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+    return codes_of(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
 }
 
 // ---- store
@@ -563,6 +562,8 @@ struct EvictArgs {
     float* W_to;
     int* kept;
     int B, Hkv, d, budget, recent;
+    int row_magic;                 // 2^20 / (d / 16) + 1: a piece's row without a division
+    __device__ __forceinline__ int by_row(int q) const { return (int)((uint32_t)q * (uint32_t)row_magic >> 20); }      // q / (d / 16), q < 2^11
 };
 
 constexpr int kSelectThreads = 1024;
@@ -682,147 +683,180 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
     }
 }
 
-// One workgroup per destination block: gathers its tokens' codes of K and V, each under its source's scale, and rounds them to
+// A workgroup per destination block and tensor: gathers its tokens' codes, each under its source's scale, and rounds them to
 // the block's own.  K's rows come straight into registers.  V's tokens lie a byte each in lines that hold a page's other tokens
-// too, so the source pages pass through LDS whole, as many at a time as gather_pages() says, and a thread picks 16 tokens of
-// a feature from there; both are held until the block's scale is known.  Bound by memory: what is kept once in and once
+// too, so the source pages pass through LDS whole, two at a time (one where they are large), and a thread picks 16 tokens of
+// a feature from there; the codes are held until the block's scale is known.  Bound by memory: what is kept once in and once
 // out, and the rest of V's source pages.
-constexpr int kGatherLds = 36 * 1024;
-constexpr int gather_page_bytes(int d, int page) { return d * (page + 4); }
-constexpr int gather_pages(int d, int page) {
-    const int n = kGatherLds / gather_page_bytes(d, page);
-    return n < 1 ? 1 : n > 8 ? 8 : n;
-}
+constexpr int gather_page_bytes(int d, int page) { return d * (page + 16); }
+constexpr int gather_pages(int d, int page) { return 2 * gather_page_bytes(d, page) <= 40 * 1024 ? 2 : 1; }
 __device__ __forceinline__ float largest_code(uint32_t w) {      // (the maximum passes over NaN)
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
     return fmaxf(fmaxf(fabsf(lo[0]), fabsf(lo[1])), fmaxf(fabsf(hi[0]), fabsf(hi[1])));
 }
-template <int NI>      // 16-byte pieces of K, and of V, per thread
+template <int NI>      // 16-byte pieces per thread
 __global__ __launch_bounds__(256) void cache_gather_kernel(EvictArgs a, int blocks) {
     extern __shared__ uint4 staged[];
     __shared__ long long src_block[128];      // page * Hkv + head
-    __shared__ int src_slot[128], src_page[128];      // slot in the source page; which of the different source pages it is
+    __shared__ int src_slot[128];             // K: slot in the source page; V: its byte among the staged rows of its round
     __shared__ int page_at[128 + 1];          // first token of each different source page
-    __shared__ float src_k[128], src_v[128];
-    __shared__ float red[2][4];
-    __shared__ int different;
+    __shared__ float src_scale[128];
+    __shared__ float red[4];
+    __shared__ int different, in_first;
     const int tid = threadIdx.x, lane = tid & 63, page = a.from.page, d = a.d;
-    const int hk = blockIdx.x % a.Hkv, j = blockIdx.x / a.Hkv % blocks, b = blockIdx.x / a.Hkv / blocks;
-    const int keep = a.to.lengths[b];
+    const int hk = blockIdx.x % a.Hkv, is_v = blockIdx.x / a.Hkv % 2, j = blockIdx.x / a.Hkv / 2 % blocks, b = blockIdx.x / a.Hkv / 2 / blocks;
+    const int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget + (long long)j * page;
+    const int* const table = a.from.table + (long long)b * a.from.max_pages;
+    // (the slots are asked for before it is known how many there are: -1 behind them)
+    const int t = tid < page && j * page + tid < a.budget ? kept[tid] : -1;
+    const int keep = a.to.lengths[b], to_page = a.to.table[(long long)b * a.to.max_pages + j];
     if (j * page >= keep) return;             // (-1: nothing)
     const int n = keep - j * page < page ? keep - j * page : page;
-    const int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget + (long long)j * page;
-    const long long size = (long long)page * d, dst = (long long)a.to.table[(long long)b * a.to.max_pages + j] * a.Hkv + hk;
-    {
-        int p = -1;
-        if (tid < n) {
-            const int t = kept[tid];
-            p = t >> a.from.log_page;
-            const long long block = (long long)a.from.table[(long long)b * a.from.max_pages + p] * a.Hkv + hk;
-            src_block[tid] = block;
-            src_slot[tid] = t & (page - 1);
-            src_k[tid] = a.from.Ks[block];
-            src_v[tid] = a.from.Vs[block];
+    const long long size = (long long)page * d, dst = (long long)to_page * a.Hkv + hk;
+    const int at_once = gather_pages(d, page), page_bytes = gather_page_bytes(d, page), pitch = page + 16;
+    const int p0 = t >> a.from.log_page;
+    float scale = 0.f;                        // (behind the last token: codes 0, which count for nothing)
+    if (tid < n) {
+        const long long block = (long long)table[p0] * a.Hkv + hk;
+        src_block[tid] = block;
+        src_slot[tid] = t & (page - 1);
+        scale = (is_v ? a.from.Vs : a.from.Ks)[block];
+    }
+    uint4 w[NI];
+    float most = 0.f;
+    if (!is_v) {
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+            const int q = p * 256 + tid, i = a.by_row(q), f = (q - i * (d / 16)) * 16;
+            w[p] = i < n ? *(const uint4*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f) : uint4{0u, 0u, 0u, 0u};
         }
+        if (tid < page) src_scale[tid] = scale;
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+            const int i = a.by_row(p * 256 + tid);
+            if (i < n) most = fmaxf(most, src_scale[i] * fmaxf(fmaxf(largest_code(w[p].x), largest_code(w[p].y)), fmaxf(largest_code(w[p].z), largest_code(w[p].w))));
+        }
+    } else {
         // tokens are in slot order: a new page begins where its number differs from the one before
         const int before = tid < n && tid > 0 ? kept[tid - 1] >> a.from.log_page : -1;
-        const unsigned long long starts = __ballot(tid < n && p != before);
-        __shared__ int in_first;
+        const unsigned long long starts = __ballot(tid < n && p0 != before);
         if (tid == 0) in_first = __popcll(starts);
         __syncthreads();
         if (tid < n) {
             const int u = __popcll(starts & (lane == 63 ? ~0ull : (2ull << lane) - 1ull)) - 1 + (tid >= 64 ? in_first : 0);
-            src_page[tid] = u;
-            if (p != before) page_at[u] = tid;
+            src_slot[tid] += u % at_once * page_bytes;
+            if (p0 != before) page_at[u] = tid;
             if (tid == n - 1) { different = u + 1; page_at[u + 1] = n; }
         }
         __syncthreads();
-    }
-    const int dp = d / 16, groups = page / 16;
-    uint4 k[NI], v[NI];
+        const int lg = a.from.log_page - 4, groups = 1 << lg, pieces = d << lg;      // 16-token groups of a feature
 #pragma unroll
-    for (int p = 0; p < NI; ++p) {
-        const int q = p * 256 + tid, i = q / dp, f = q % dp * 16;
-        k[p] = i < n ? *(const uint4*)(a.from.K + src_block[i] * size + (long long)src_slot[i] * d + f) : uint4{0u, 0u, 0u, 0u};
-        v[p] = uint4{0u, 0u, 0u, 0u};
-    }
-    const int pitch = page + 4, at_once = gather_pages(d, page), pieces = d * groups;
-    for (int u0 = 0; u0 < different; u0 += at_once) {
-        const int u1 = u0 + at_once < different ? u0 + at_once : different;
-        if (u0) __syncthreads();
-        for (int q = tid; q < (u1 - u0) * pieces; q += 256) {
-            const int u = q / pieces, r = q % pieces, g = r % groups * 16, f = r / groups;
-            const uint4 w = *(const uint4*)(a.from.V + src_block[page_at[u0 + u]] * size + (long long)f * page + g);
-            uint32_t* const to = (uint32_t*)((uint8_t*)staged + u * gather_page_bytes(d, page) + f * pitch + g);
-            to[0] = w.x; to[1] = w.y; to[2] = w.z; to[3] = w.w;
+        for (int p = 0; p < NI; ++p) w[p] = uint4{0u, 0u, 0u, 0u};
+        // a round's source pages are asked for while the round before is picked from
+        uint4 x0[NI], x1[NI];
+        auto page_of_round = [&](int u, uint4 (&x)[NI]) {
+            const uint8_t* const src = a.from.V + src_block[page_at[u < different ? u : 0]] * size;
+#pragma unroll
+            for (int p = 0; p < NI; ++p) {
+                const int q = p * 256 + tid;
+                x[p] = q < pieces && u < different ? *(const uint4*)(src + q * 16) : uint4{0u, 0u, 0u, 0u};
+            }
+        };
+        auto put = [&](int u, const uint4 (&x)[NI]) {
+#pragma unroll
+            for (int p = 0; p < NI; ++p) {
+                const int q = p * 256 + tid, g = (q & (groups - 1)) * 16, f = q >> lg;
+                if (q < pieces) *(uint4*)((uint8_t*)staged + u * page_bytes + f * pitch + g) = x[p];
+            }
+        };
+        page_of_round(0, x0);
+        if (at_once == 2) page_of_round(1, x1);
+        for (int u0 = 0; u0 < different; u0 += at_once) {
+            const int u1 = u0 + at_once < different ? u0 + at_once : different;
+            if (u0) __syncthreads();
+            put(0, x0);
+            if (u1 - u0 == 2) put(1, x1);
+            page_of_round(u1, x0);
+            if (at_once == 2) page_of_round(u1 + 1, x1);
+            if (u0 == 0 && tid < page) src_scale[tid] = scale;
+            __syncthreads();
+            const int i0 = page_at[u0], i1 = page_at[u1];
+#pragma unroll
+            for (int p = 0; p < NI; ++p) {
+                const int q = p * 256 + tid, g = (q & (groups - 1)) * 16, f = q >> lg;
+                if (q >= pieces || g >= i1 || g + 16 <= i0) continue;
+                const uint8_t* const src = (const uint8_t*)staged + f * pitch;
+                if (g >= i0 && g + 16 <= i1) {       // (most are: no token of the 16 in another round)
+                    uint32_t c[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const int4 at = *(const int4*)(src_slot + g + e);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) c[e + h] = src[(&at.x)[h]];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) (&w[p].x)[e / 4] = c[e] | c[e + 1] << 8 | c[e + 2] << 16 | c[e + 3] << 24;
+                    continue;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const int4 at = *(const int4*)(src_slot + g + e);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (g + e + h >= i0 && g + e + h < i1) (&w[p].x)[e / 4] |= (uint32_t)src[(&at.x)[h]] << (8 * h);
+                }
+            }
         }
-        __syncthreads();
-        const int i0 = page_at[u0], i1 = page_at[u1];
 #pragma unroll
         for (int p = 0; p < NI; ++p) {
-            const int q = p * 256 + tid, f = q % d, g = q / d * 16;
-            if (g >= page || g >= i1 || g + 16 <= i0) continue;
-            const uint8_t* const src = (const uint8_t*)staged + f * pitch;
+            const int g = ((p * 256 + tid) & (groups - 1)) * 16;
+            if (g >= n) continue;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = g + e;
-                if (i >= i0 && i < i1) (&v[p].x)[e / 4] |= (uint32_t)src[(src_page[i] - u0) * gather_page_bytes(d, page) + src_slot[i]] << (8 * (e & 3));
+            for (int e = 0; e < 16; e += 4) {
+                const float4 s = *(const float4*)(src_scale + g + e);
+                const uint32_t x = (&w[p].x)[e / 4];
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+                most = fmaxf(fmaxf(most, fmaxf(fabsf(lo[0]) * s.x, fabsf(lo[1]) * s.y)), fmaxf(fabsf(hi[0]) * s.z, fabsf(hi[1]) * s.w));
             }
         }
     }
-    float mk = 0.f, mv = 0.f;
-#pragma unroll
-    for (int p = 0; p < NI; ++p) {
-        const int q = p * 256 + tid, i = q / dp, g = q / d * 16;
-        if (i < n) mk = fmaxf(mk, src_k[i] * fmaxf(fmaxf(largest_code(k[p].x), largest_code(k[p].y)), fmaxf(largest_code(k[p].z), largest_code(k[p].w))));
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            if (g + e < n) {
-                const uint32_t c = ((&v[p].x)[e / 4] >> (8 * (e & 3))) & 0xffu;
-                mv = fmaxf(mv, src_v[g + e] * fabsf(__builtin_amdgcn_cvt_pk_f32_fp8((int)c, false)[0]));
-            }
-    }
-    mk = wave_max(mk);
-    mv = wave_max(mv);
-    if (lane == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
+    most = wave_max(most);
+    if (lane == 0) red[tid >> 6] = most;
     __syncthreads();
-    mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-    mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
-    const int ek = scale_exponent(mk), ev = scale_exponent(mv);
-    if (tid == 0) { a.to.Ks[dst] = pow2f(ek); a.to.Vs[dst] = pow2f(ev); }
-    const float ik = pow2f(-ek), iv = pow2f(-ev);
+    const int ex = scale_exponent(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+    if (tid == 0) (is_v ? a.to.Vs : a.to.Ks)[dst] = pow2f(ex);
+    const float inv = pow2f(-ex);
+    if (!is_v) {
+#pragma unroll
+        for (int p = 0; p < NI; ++p) {
+            const int q = p * 256 + tid, i = a.by_row(q);
+            if (i >= n) continue;
+            const float s = src_scale[i] * inv;
+            if (s != 1.f) w[p] = uint4{rescale_codes(w[p].x, s), rescale_codes(w[p].y, s), rescale_codes(w[p].z, s), rescale_codes(w[p].w, s)};
+            ((uint4*)(a.to.K + dst * size))[q] = w[p];
+        }
+        return;
+    }
+    const int lg = a.from.log_page - 4, groups = 1 << lg, pieces = d << lg;
 #pragma unroll
     for (int p = 0; p < NI; ++p) {
-        const int q = p * 256 + tid, i = q / dp;
-        if (i < n) {
-            const float s = src_k[i] * ik;
-            uint4 w = k[p];
-            if (s != 1.f) w = uint4{rescale_codes(w.x, s), rescale_codes(w.y, s), rescale_codes(w.z, s), rescale_codes(w.w, s)};
-            *(uint4*)(a.to.K + dst * size + (long long)i * d + q % dp * 16) = w;
-        }
-        const int f = q % d, g = q / d * 16;
-        if (g >= n) continue;
-        uint4 w = v[p];
+        const int q = p * 256 + tid, g = (q & (groups - 1)) * 16;
+        if (q >= pieces || g >= n) continue;
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            uint32_t& x = (&w.x)[e / 4];
-            float s[4];
-            bool same = true;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                s[h] = src_v[g + e + h < n ? g + e + h : n - 1] * iv;
-                same &= s[h] == 1.f;
-            }
-            if (same) continue;
+            uint32_t& x = (&w[p].x)[e / 4];
+            const float4 s = *(const float4*)(src_scale + g + e);
             const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
-            x = to_codes(lo[0] * s[0], lo[1] * s[1], hi[0] * s[2], hi[1] * s[3]);
+            x = codes_of(lo[0] * (s.x * inv), lo[1] * (s.y * inv), hi[0] * (s.z * inv), hi[1] * (s.w * inv));
         }
-        uint8_t* const out = a.to.V + dst * size + (long long)f * page + g;
-        if (g + 16 <= n) *(uint4*)out = w;
+        uint8_t* const out = a.to.V + dst * size + q * 16;
+        if (g + 16 <= n) *(uint4*)out = w[p];
         else {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                if (g + e < n) out[e] = (uint8_t)((&w.x)[e / 4] >> (8 * (e & 3)));
+                if (g + e < n) out[e] = (uint8_t)((&w[p].x)[e / 4] >> (8 * (e & 3)));
         }
     }
 }

@@ -44,7 +44,7 @@ hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st) {
     const hipError_t e = launch(cache_select_kernel, (long long)a.B * a.Hkv, kSelectThreads, 0, st, a);
     if (e != hipSuccess) return e;
     const int items = (a.d * a.from.page / 16 + 255) / 256, lds_bytes = gather_pages(a.d, a.from.page) * gather_page_bytes(a.d, a.from.page);
-    const long long grid = (long long)a.B * blocks * a.Hkv;
+    const long long grid = (long long)a.B * blocks * 2 * a.Hkv;
 #define CSAT_GATHER(NI_) launch(cache_gather_kernel<NI_>, grid, 256, lds_bytes, st, a, blocks)
     return items <= 1 ? CSAT_GATHER(1) : items <= 2 ? CSAT_GATHER(2) : items <= 4 ? CSAT_GATHER(4) : CSAT_GATHER(8);
 #undef CSAT_GATHER

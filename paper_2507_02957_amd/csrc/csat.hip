@@ -2188,15 +2188,19 @@ csat_status check_packed(const csat_packed_dims* d, int d_multiple) {
 int longest_q(const csat_packed_dims& d) { return std::min(d.max_q, d.n_q); }
 int longest_k(const csat_packed_dims& d) { return std::min(d.max_k, d.n_k); }
 
-struct PromptPlan { int tiles, shares; size_t bytes; };
-// Row tiles of 128; the keys in shares where the tiles leave most of the chip idle, a share no shorter than 256 keys.
+struct PromptPlan { bool split; int tiles, shares; size_t bytes; };
+// Row tiles of 128, or of 32 whose keys the wavefronts divide: float always, bf16 where tiles of 128 would occupy less than half
+// of the compute units (8 heads x 512 rows, d 64, 32 tiles of 128: 7.5 against 11.9 us; 2 key heads x 1024 x 4, d 128, 64 tiles: 15.7
+// against 25.5; not 96 heads x 274, 288 tiles: 15.5 against 11.7, nor 4 x 2048 x 4, 256 tiles: 60 against 47).  The keys in shares where even
+// then tiles are fewer than compute units, a share no shorter than 256 keys (one row of 32 heads against 4096 keys: 12.2
+// against 38.8 us; 1024 rows, d 256, 32 tiles of 128: 25.6 against 27.0).
 PromptPlan prompt_plan(const csat_packed_dims& d) {
     PromptPlan p{};
     const int G = d.Hq / d.Hkv;
-    const long long rows = (long long)longest_q(d) * G;
-    p.tiles = (int)((rows + 127) / 128);
-    const long long groups = (long long)d.B * d.Hkv * p.tiles;
-    p.shares = (int)std::max(1LL, std::min<long long>(512 / groups, longest_k(d) / 256));
+    const long long rows = (long long)longest_q(d) * G, pairs = (long long)d.B * d.Hkv;
+    p.split = d.dtype == CSAT_F32 || pairs * ((rows + 127) / 128) < 128;
+    p.tiles = (int)(p.split ? (rows + 31) / 32 : (rows + 127) / 128);
+    p.shares = (int)std::max(1LL, std::min<long long>(256 / (pairs * p.tiles), longest_k(d) / 256));
     p.bytes = p.shares > 1 ? (size_t)p.shares * d.n_q * d.Hq * (d.d + 2) * 4 : 0;
     return p;
 }
@@ -2223,13 +2227,15 @@ CacheView cache_view(const csat_cache& c) {
 }
 
 struct CachedPlan { int tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; };
-// Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike.
-constexpr int kShareTokens = 512;
+// Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike: 512, more where a
+// sequence would have more shares than it takes to occupy the chip twice (one sequence of 131072 tokens, 8 key heads: 58 us with
+// shares of 2048, 63, 72, 92 with 1024, 512, 256, whose join grows; 32 sequences of 700 to 8100: 92 us with 512, 100 with 2048).
 CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weights) {
     CachedPlan p{};
     const long long rows = (long long)longest_q(d) * (d.Hq / d.Hkv);
     p.tiles = (int)((rows + 15) / 16);
-    p.share_tokens = getenv("CSAT_SHARE") ? atoi(getenv("CSAT_SHARE")) : kShareTokens;
+    const long long groups = (long long)d.B * d.Hkv * p.tiles, most = std::max({512 / groups, std::min(64LL, 8192 / groups), 16LL});
+    p.share_tokens = (int)std::max(512LL, round_up((c.max_len + most - 1) / most, 256));
     p.shares = (c.max_len + p.share_tokens - 1) / p.share_tokens;
     p.score_ld = (int)round_up(c.max_len, 64);
     p.part_bytes = p.shares > 1 || weights ? (size_t)round_up((long long)p.shares * d.n_q * d.Hq * (d.d + 2) * 4, 256) : 0;
@@ -2833,7 +2839,7 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     a.sl = scale * 1.4426950408889634f;
     a.tiles = p.tiles; a.shares = p.shares; a.part = (float*)workspace;
     Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_PROMPT, st);
-    HIP_TRY(d.dtype == CSAT_BF16 ? prompt_launch_bf16(a, st) : prompt_launch_f32(a, st));
+    HIP_TRY(d.dtype == CSAT_BF16 ? prompt_launch_bf16(a, p.split, st) : prompt_launch_f32(a, p.split, st));
     if (p.shares > 1) {
         tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
         JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares, nullptr, 0, 0};

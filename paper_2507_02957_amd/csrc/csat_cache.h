@@ -491,7 +491,7 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     }
 }
 
-// The second launch: the first o_blocks workgroups join a row of O each, the others form W = decay W + sum over rows of
+// The second launch: the first o_blocks workgroups join the rows of O, the others form W = decay W + sum over rows of
 // 2^(score - lse) for 1024 tokens of a sequence and key head, a thread four of them.
 template <typename T>
 __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs a, int o_blocks) {
@@ -499,8 +499,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
     __shared__ float lse2[RB];
     __shared__ int limit[RB];
     if ((int)blockIdx.x < o_blocks) {
-        const int per = j.max_q * j.Hq;
-        join_row<T>(j, blockIdx.x / per, blockIdx.x % per);
+        join_block<T>(j, blockIdx.x);
         return;
     }
     const int tid = threadIdx.x, lane = tid & 63;

@@ -60,10 +60,10 @@ hipError_t attention_z_launch(int d, int parts, bool resident, const AttentionZA
 constexpr int kListaSupportMaxN = 4096;
 hipError_t lista_support_launch(const ListaSupportArgs& a, unsigned grid, hipStream_t st);
 
-// Exact attention over packed sequences (csat_prompt.h), and the join of the shares of its keys; csat_tu_prompt.hip compiled
+// Exact attention over packed sequences (csat_prompt.h; split: the form whose workgroups have 32 rows, the only one for float), and the join of the shares of its keys; csat_tu_prompt.hip compiled
 // with -DCSAT_TU_BF16=<0|1>.
-hipError_t prompt_launch_bf16(const PromptArgs& a, hipStream_t st);
-hipError_t prompt_launch_f32(const PromptArgs& a, hipStream_t st);
+hipError_t prompt_launch_bf16(const PromptArgs& a, bool split, hipStream_t st);
+hipError_t prompt_launch_f32(const PromptArgs& a, bool split, hipStream_t st);
 hipError_t attention_join_launch_bf16(const JoinArgs& a, hipStream_t st);
 hipError_t attention_join_launch_f32(const JoinArgs& a, hipStream_t st);
 

@@ -24,15 +24,12 @@ struct PromptArgs {
     int B, Hq, Hkv, G, d, n_q, n_k, max_q, causal;
     float sl;                      // scale log2(e)
     int tiles;                     // row tiles per sequence and key head
-    int shares;                    // > 1: workgroups that split a row tile's keys, joined by prompt_join_kernel
+    int shares;                    // > 1: workgroups that split a row tile's keys, joined by attention_join_kernel
     float* part;                   // [shares][n_q Hq][d] unnormalised outputs, then [shares][n_q Hq][2]: offset, sum
 };
 
 constexpr int kPromptWaves = 4;
-template <typename T> constexpr int prompt_key_tiles() { return sizeof(T) == 2 ? 2 : 1; }      // 32-key tiles per step
-template <typename T, int DT> constexpr int prompt_lds_bytes() {
-    return 2 * 2 * prompt_key_tiles<T>() * 32 * DT * 32 * (int)sizeof(T) + 32 * DT * 12 + 16;      // K and V twice; three keys a column, a word
-}
+template <int DT> constexpr int prompt_lds() { return 2 * 2 * 64 * DT * 32 * 2 + 32 * DT * 12 + 16; }      // K and V twice; three keys a column, a word
 
 // One sequence's rows: clamped to the tensors whatever the offsets say.
 struct PackedSpan {
@@ -110,129 +107,51 @@ template <typename T, int C> __device__ __forceinline__ int swizzle_v(int row) {
     return C % 16 == 0 ? 4 * (row & 3) : C % 8 == 0 ? 4 * ((row >> 1) & 1) : 0;
 }
 
-template <typename T, int DT, int NT>
-__global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-    typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
-    typedef __attribute__((address_space(3))) const float* lds_float;
-    constexpr bool BF = sizeof(T) == 2;
-    constexpr int KT = prompt_key_tiles<T>(), KEYS = 32 * KT, D = 32 * DT, THREADS = 64 * kPromptWaves;
-    constexpr int EPC = Elem<T>::per_chunk, C = D / EPC, NK = C / 2;      // 16-byte pieces of a row, pairs of them
-    constexpr int PIECES = KEYS * C / THREADS, TILE = KEYS * C * 16;
-    static_assert(KEYS * C % THREADS == 0, "a step's pieces are dealt out evenly");
-    extern __shared__ uint4 lds[];                  // K tile, V tile; the same once more; then the columns' odd values
-    OddColumn* const oddc = (OddColumn*)(lds + 4 * KEYS * C);
-    int* const any_odd = (int*)(oddc + D);
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-
-    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // the last row tiles, which see most keys, first; neighbouring workgroups take different heads, so an XCD's keep to a
-    // share of the heads where their number is a multiple of eight
-    const int P = a.B * a.Hkv;
-    const int share = blockIdx.x / (P * a.tiles), id = blockIdx.x % (P * a.tiles);
-    const int pair = id % P, tile = a.tiles - 1 - id / P;
-    const int b = pair / a.Hkv, hk = pair % a.Hkv;
-    const PackedSpan qs(a.q_off, b, a.n_q), ks(a.k_off, b, a.n_k);
-    const int nk = ks.count, rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G;
-    const int r_base = tile * (32 * NT * kPromptWaves);
-    if (r_base >= rows) return;
-    auto limit_of = [&](int r) {      // keys that row r sees
-        if (!a.causal) return nk;
-        const int v = r / a.G + nk - qs.count + 1;
-        return v < 0 ? 0 : v > nk ? nk : v;
-    };
-    const int r_end = r_base + 32 * NT * kPromptWaves < rows ? r_base + 32 * NT * kPromptWaves : rows;
-    const int lo = limit_of(r_base), hi = limit_of(r_end - 1);
-    const int steps = (hi + KEYS - 1) / KEYS;
-    const int t0 = (int)((long long)steps * share / a.shares), t1 = (int)((long long)steps * (share + 1) / a.shares);
-
-    // this wavefront's rows
-    const int w_base = r_base + wave * 32 * NT;
-    const bool active = w_base < rows;
-    const int w_end = w_base + 32 * NT < rows ? w_base + 32 * NT : rows;
-    const int w_lo = active ? limit_of(w_base) : 0, w_hi = active ? limit_of(w_end - 1) : 0;
-    int lim[NT];
+// What a wavefront keeps of NT x 32 rows and does with KT x 32 keys in LDS.
+template <typename T, int DT, int NT, int KT>
+struct PromptRows {
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr int D = 32 * DT, EPC = Elem<T>::per_chunk, C = D / EPC, NK = C / 2;      // 16-byte pieces of a row, pairs of them
     uint4 qf[NT][NK];
-    const int dc = a.d / EPC;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        int r = w_base + 32 * n + li;
-        if (r >= rows) r = rows - 1;
-        lim[n] = limit_of(r);
-        const T* q = (const T*)a.Q + (long long)(qs.first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
-#pragma unroll
-        for (int g = 0; g < NK; ++g) {
-            const int c = 2 * g + lh;
-            qf[n][g] = c < dc ? *(const uint4*)(q + c * EPC) : uint4{0u, 0u, 0u, 0u};
-        }
-    }
     f32x16 o[NT][DT];
-    float ref[NT], off[NT], sum[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        ref[n] = -INFINITY; off[n] = 0.f; sum[n] = 0.f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[n][t][v] = 0.f;
-    }
-    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
-    if (tid == 0) *any_odd = 0;
+    float ref[NT], off[NT], sum[NT];      // reference score, what a weight's exponent takes off for it, this lane's share of the row's sum
+    int lim[NT];                          // keys that the lane's row sees
 
-    // A step's pieces go from memory straight into LDS, piece q of the tile at its place there; a thread's pieces q = 256 p + tid
-    // come from the places that the swizzles send there (token strides are below 2^24 elements, so 32 bits hold them within a
-    // step).  Rows behind the sequence's last one are that one again (masked); columns behind d are zeroed once and left out.
-    const char* const kb = (const char*)a.K + ((long long)ks.first * a.k_token + (long long)hk * a.k_head) * (long long)sizeof(T);
-    const char* const vb = (const char*)a.V + ((long long)ks.first * a.v_token + (long long)hk * a.v_head) * (long long)sizeof(T);
-    const uint32_t k_row = (uint32_t)a.k_token * (uint32_t)sizeof(T), v_row = (uint32_t)a.v_token * (uint32_t)sizeof(T);
-    uint32_t ko[PIECES], vo[PIECES];
+    // rows base .. of `rows` (beyond them the last one)
+    template <typename Limit>
+    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int base, int rows, int lane, Limit limit_of) {
+        const int li = lane & 31, lh = lane >> 5, dc = a.d / EPC;
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        const int q = p * THREADS + tid, row = q / C, c = q % C;
-        ko[p] = (uint32_t)row * k_row + 16u * (uint32_t)(c ^ swizzle_k<C>(row));
-        vo[p] = (uint32_t)row * v_row + 16u * (uint32_t)(c ^ swizzle_v<T, C>(row));
-    }
-    if (dc < C)
-        for (int i = tid; i < 4 * KEYS * C; i += THREADS) lds[i] = uint4{0u, 0u, 0u, 0u};
-    auto load = [&](int t) {
-        const char* const kt = kb + (long long)t * KEYS * k_row;
-        const char* const vt = vb + (long long)t * KEYS * v_row;
-        const uint32_t at = lds0 + (t & 1) * 2 * TILE + wave * 1024;
-        if (dc == C && (t + 1) * KEYS <= nk) {
+        for (int n = 0; n < NT; ++n) {
+            int r = base + 32 * n + li;
+            if (r >= rows) r = rows - 1;
+            lim[n] = limit_of(r);
+            const T* q = (const T*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
+            if (dc == C) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) stage16(at + p * THREADS * 16, kt, ko[p]);
+                for (int g = 0; g < NK; ++g) qf[n][g] = *(const uint4*)(q + (2 * g + lh) * EPC);
+            } else {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) stage16(at + TILE + p * THREADS * 16, vt, vo[p]);
-            return;
-        }
-        const int left = nk - 1 - t * KEYS;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int q = p * THREADS + tid, row = q / C, c = q % C, over = row > left ? row - left : 0;
-            if ((c ^ swizzle_k<C>(row)) < dc) stage16(at + p * THREADS * 16, kt, ko[p] - (uint32_t)over * k_row);
-            if ((c ^ swizzle_v<T, C>(row)) < dc) stage16(at + TILE + p * THREADS * 16, vt, vo[p] - (uint32_t)over * v_row);
-        }
-    };
-    __syncthreads();                                 // (the zeroed columns, and the columns' odd values are set up)
-    if (t0 < t1) load(t0);
-    for (int t = t0; t < t1; ++t) {
-        const uint32_t sk = lds0 + (t & 1) * 2 * TILE, sv = sk + TILE;
-        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this thread's pieces are there
-        __syncthreads();                             // ... and everybody's; the other half of the LDS has been read
-        if (t + 1 < t1) load(t + 1);
-        if ((t + 1) * KEYS > lo) {                   // some row of the workgroup does not see all of the step's keys
-            uint4* const wv = lds + (t & 1) * 2 * KEYS * C + KEYS * C;
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                const int q = p * THREADS + tid, row = q / C, c = q % C ^ swizzle_v<T, C>(row);
-                take_odd<T>(wv + q, t * KEYS + row, oddc + c * EPC, any_odd);
+                for (int g = 0; g < NK; ++g) {
+                    const int c = 2 * g + lh;
+                    qf[n][g] = c < dc ? *(const uint4*)(q + c * EPC) : uint4{0u, 0u, 0u, 0u};
+                }
             }
-            __syncthreads();
+            ref[n] = -INFINITY; off[n] = 0.f; sum[n] = 0.f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[n][t][v] = 0.f;
         }
-        if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
+    }
 
+    // keys key0 .., K's tile at LDS address sk, V's at sv; masked: some row does not see all of them
+    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+        typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
+        typedef __attribute__((address_space(3))) const float* lds_float;
+        const int li = lane & 31, lh = lane >> 5;
         f32x16 s[NT][KT];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -248,14 +167,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
 #pragma unroll
                 for (int n = 0; n < NT; ++n) mfma_group<T>(__builtin_bit_cast(uint4, kf), qf[n][g], s[n][u]);
             }
-        if ((t + 1) * KEYS > w_lo) {
+        if (masked) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int u = 0; u < KT; ++u)
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        if (t * KEYS + 32 * u + 8 * (v >> 2) + 4 * lh + (v & 3) >= lim[n]) s[n][u][v] = -INFINITY;
+                        if (key0 + 32 * u + 8 * (v >> 2) + 4 * lh + (v & 3) >= lim[n]) s[n][u][v] = -INFINITY;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -265,9 +184,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
 #pragma unroll
                 for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[n][u][v]);
             mx = pair_max(mx);
-            if (__builtin_amdgcn_ballot_w64((mx - ref[n]) * a.sl > 8.f) != 0) {      // (both lanes of a pair agree; -inf against -inf is no)
+            if (__builtin_amdgcn_ballot_w64((mx - ref[n]) * sl > 8.f) != 0) {      // (both lanes of a pair agree; -inf against -inf is no)
                 // before a row's first score there is nothing to rescale, and no offset that means anything
-                const float nm = fmaxf(mx, ref[n]), to = nm == -INFINITY ? 0.f : -nm * a.sl;
+                const float nm = fmaxf(mx, ref[n]), to = nm == -INFINITY ? 0.f : -nm * sl;
                 const float f = ref[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off[n]);
                 ref[n] = nm;
                 off[n] = to;
@@ -281,7 +200,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
             for (int u = 0; u < KT; ++u)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    s[n][u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][u][v], a.sl, off[n]));
+                    s[n][u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][u][v], sl, off[n]));
                     sum[n] += s[n][u][v];
                 }
         }
@@ -325,70 +244,301 @@ __global__ __launch_bounds__(64 * kPromptWaves, NT == 1 && DT <= 4 ? 2 : 1) void
             }
         }
     }
+};
+
+// A sequence's keys in steps of KEYS: a step's pieces go from memory straight into LDS, piece q of the tile at its place there;
+// thread `tid` of THREADS brings the pieces q = THREADS p + tid from the places that the swizzles send there (token strides are
+// below 2^24 elements, so 32 bits hold them within a step).  Rows behind the sequence's last one are that one again
+// (masked); columns behind d are left out (zeroed beforehand).
+template <typename T, int C, int KEYS, int THREADS>
+struct PromptKeys {
+    static constexpr int PIECES = KEYS * C / THREADS, TILE = KEYS * C * 16;
+    static_assert(KEYS * C % THREADS == 0, "a step's pieces are dealt out evenly");
+    const char *kb, *vb;
+    uint32_t k_row, v_row;
+    uint32_t ko[PIECES], vo[PIECES];
+    int nk, dc;
+    __device__ __forceinline__ PromptKeys(const PromptArgs& a, int first, int count, int hk, int tid) : nk(count), dc(a.d / Elem<T>::per_chunk) {
+        kb = (const char*)a.K + ((long long)first * a.k_token + (long long)hk * a.k_head) * (long long)sizeof(T);
+        vb = (const char*)a.V + ((long long)first * a.v_token + (long long)hk * a.v_head) * (long long)sizeof(T);
+        k_row = (uint32_t)a.k_token * (uint32_t)sizeof(T);
+        v_row = (uint32_t)a.v_token * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int q = p * THREADS + tid, row = q / C, c = q % C;
+            ko[p] = (uint32_t)row * k_row + 16u * (uint32_t)(c ^ swizzle_k<C>(row));
+            vo[p] = (uint32_t)row * v_row + 16u * (uint32_t)(c ^ swizzle_v<T, C>(row));
+        }
+    }
+    // step t: K's tile to LDS address `at`, V's behind it; `wave`: which 64 of the threads this wavefront is
+    __device__ __forceinline__ void load(int t, uint32_t at, int wave, int tid) const {
+        const char* const kt = kb + (long long)t * KEYS * k_row;
+        const char* const vt = vb + (long long)t * KEYS * v_row;
+        at += wave * 1024;
+        if (dc == C && (t + 1) * KEYS <= nk) {
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) stage16(at + p * THREADS * 16, kt, ko[p]);
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) stage16(at + TILE + p * THREADS * 16, vt, vo[p]);
+            return;
+        }
+        const int left = nk - 1 - t * KEYS;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int q = p * THREADS + tid, row = q / C, c = q % C, over = row > left ? row - left : 0;
+            if ((c ^ swizzle_k<C>(row)) < dc) stage16(at + p * THREADS * 16, kt, ko[p] - (uint32_t)over * k_row);
+            if ((c ^ swizzle_v<T, C>(row)) < dc) stage16(at + TILE + p * THREADS * 16, vt, vo[p] - (uint32_t)over * v_row);
+        }
+    }
+    // zeros where load() leaves out the columns behind d, of `tiles` tiles from `to` (K and V in turn)
+    __device__ __forceinline__ void clear(uint4* to, int tiles, int tid) const {
+        for (int u = 0; u < tiles; ++u)
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                const int q = p * THREADS + tid, row = q / C, c = q % C;
+                if ((c ^ (u & 1 ? swizzle_v<T, C>(row) : swizzle_k<C>(row))) >= dc) to[u * KEYS * C + q] = uint4{0u, 0u, 0u, 0u};
+            }
+    }
+    // the odd values of V's staged tile (see take_odd)
+    __device__ __forceinline__ void look_over(int t, uint4* sv, int tid, OddColumn* oddc, int* any_odd) const {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int q = p * THREADS + tid, row = q / C, c = q % C ^ swizzle_v<T, C>(row);
+            take_odd<T>(sv + q, t * KEYS + row, oddc + c * Elem<T>::per_chunk, any_odd);
+        }
+    }
+};
+__device__ __forceinline__ void wait_staged() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0): this wavefront's pieces are there
+
+// Which rows a workgroup has.  Of `tiles` row tiles of ROWS the last, which see most keys, come first; neighbouring workgroups
+// take different heads, so an XCD's keep to a share of the heads where their number is a multiple of eight.
+template <int ROWS>
+struct PromptPlace {
+    int share, b, hk, r_base, rows, r_end, lo, hi, q_first, q_count, k_first, nk, G, causal;
+    __device__ __forceinline__ explicit PromptPlace(const PromptArgs& a) {
+        const int P = a.B * a.Hkv, id = blockIdx.x % (P * a.tiles), pair = id % P;
+        share = blockIdx.x / (P * a.tiles);
+        b = pair / a.Hkv;
+        hk = pair % a.Hkv;
+        G = a.G;
+        causal = a.causal;
+        const PackedSpan qs(a.q_off, b, a.n_q), ks(a.k_off, b, a.n_k);
+        q_first = qs.first; q_count = qs.count; k_first = ks.first; nk = ks.count;
+        rows = (q_count < a.max_q ? q_count : a.max_q) * G;
+        r_base = (a.tiles - 1 - id / P) * ROWS;
+        r_end = r_base + ROWS < rows ? r_base + ROWS : rows;
+        lo = r_base < rows ? limit(r_base) : 0;
+        hi = r_base < rows ? limit(r_end - 1) : 0;
+    }
+    // this workgroup's steps of the keys, KEYS each
+    template <int KEYS>
+    __device__ __forceinline__ void steps(int shares, int* t0, int* t1) const {
+        const int n = (hi + KEYS - 1) / KEYS;
+        *t0 = 0;
+        *t1 = n;
+        if (shares == 1) return;
+        const int per = (int)((uint32_t)(n + shares - 1) / (uint32_t)shares);
+        *t0 = share * per < n ? share * per : n;
+        *t1 = *t0 + per < n ? *t0 + per : n;
+    }
+    __device__ __forceinline__ int limit(int r) const {      // keys that row r sees
+        if (!causal) return nk;
+        const int v = r / G + nk - q_count + 1;
+        return v < 0 ? 0 : v > nk ? nk : v;
+    }
+};
+
+// Long sequences, bf16: four wavefronts of 32 rows each go over the same keys, 64 at a time, which they stage together, the next step's
+// while one is worked on.  Two wavefronts per SIMD fill each other's waits between products (32 a step), exponentials (32 at a
+// quarter of the rate) and fragment reads (32 KB a step, at 128 bytes a cycle and CU just below the products' time).
+template <int DT>
+__global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+    typedef bf16_t T;
+    typedef PromptRows<T, DT, 1, 2> Rows;
+    constexpr int C = Rows::C, D = Rows::D, KEYS = 64, THREADS = 64 * kPromptWaves;
+    typedef PromptKeys<T, C, KEYS, THREADS> Keys;
+    extern __shared__ uint4 lds[];                  // K tile, V tile; the same once more; then the columns' odd values
+    OddColumn* const oddc = (OddColumn*)(lds + 4 * KEYS * C);
+    int* const any_odd = (int*)(oddc + D);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const PromptPlace<32 * kPromptWaves> at(a);
+    if (at.r_base >= at.rows) return;
+    const int w_base = at.r_base + wave * 32;
+    const bool active = w_base < at.rows;
+    const int w_end = w_base + 32 < at.rows ? w_base + 32 : at.rows;
+    const int w_lo = active ? at.limit(w_base) : 0, w_hi = active ? at.limit(w_end - 1) : 0;
+    int t0, t1;
+    at.steps<KEYS>(a.shares, &t0, &t1);
+    const Keys keys(a, at.k_first, at.nk, at.hk, tid);
+    if (t0 < t1) keys.load(t0, lds0 + (t0 & 1) * 2 * Keys::TILE, wave, tid);
+    if (keys.dc < C) keys.clear(lds, 4, tid);
+    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
+    if (tid == 0) *any_odd = 0;
+    Rows rows;
+    rows.init(a, at.q_first, at.hk, w_base, at.rows, lane, [&](int r) { return at.limit(r); });
+    for (int t = t0; t < t1; ++t) {
+        const uint32_t sk = lds0 + (t & 1) * 2 * Keys::TILE;
+        wait_staged();
+        __syncthreads();                             // everybody's pieces are there; the other half of the LDS has been read
+        if (t + 1 < t1) keys.load(t + 1, lds0 + ((t + 1) & 1) * 2 * Keys::TILE, wave, tid);
+        if ((t + 1) * KEYS > at.lo) {                // some row of the workgroup does not see all of the step's keys
+            keys.look_over(t, lds + (t & 1) * 2 * KEYS * C + KEYS * C, tid, oddc, any_odd);
+            __syncthreads();
+        }
+        if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
+        rows.step(sk, sk + Keys::TILE, t * KEYS, (t + 1) * KEYS > w_lo, a.sl, lane);
+    }
     __syncthreads();                                 // (the last steps' odd values are noted)
     if (!active) return;
-    const bool odd = *any_odd != 0;
 
+    const float total = pair_sum(rows.sum[0]);
+    const bool ok = w_base + li < at.rows;
+    const int r = ok ? w_base + li : at.rows - 1, head = at.hk * a.G + r % a.G;
+    const long long row = at.q_first + r / a.G;
+    f32x16 (&o)[DT] = rows.o[0];
+    if (*any_odd) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const float total = pair_sum(sum[n]);
-        const int r = w_base + 32 * n + li;
-        const bool ok = r < rows;
-        const int rr = ok ? r : rows - 1, head = hk * a.G + rr % a.G;
-        const long long row = qs.first + rr / a.G;
-        if (odd) {
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+            for (int v = 0; v < 16; ++v) o[dt][v] = with_odd(o[dt][v], oddc[32 * dt + 8 * (v >> 2) + 4 * lh + (v & 3)], rows.lim[0]);
+    }
+    if (a.shares > 1) {
+        const long long all = (long long)a.n_q * a.Hq, p0 = (long long)at.share * all + row * a.Hq + head;
+        if (!ok) return;
+        float* p = a.part + p0 * a.d;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) o[n][dt][v] = with_odd(o[n][dt][v], oddc[32 * dt + 8 * (v >> 2) + 4 * lh + (v & 3)], lim[n]);
-        }
-        if (a.shares > 1) {
-            const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + head;
-            if (ok) {
-                float* p = a.part + at * a.d;
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int col = 32 * dt + 8 * g + 4 * lh;
-                        if (col < a.d) *(float4*)(p + col) = float4{o[n][dt][4 * g], o[n][dt][4 * g + 1], o[n][dt][4 * g + 2], o[n][dt][4 * g + 3]};
-                    }
-                float2* ml = (float2*)(a.part + (long long)a.shares * all * a.d) + at;
-                if (lh == 0) *ml = float2{total == 0.f ? INFINITY : off[n], total};
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * dt + 8 * g + 4 * lh;
+                if (col < a.d) *(float4*)(p + col) = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
             }
-            continue;
-        }
-        const float inv = total == 0.f ? 0.f : 1.f / total;      // (a row that saw nothing is 0)
-        if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off[n]);
-        T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head;
+        if (lh == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[p0] = float2{total == 0.f ? INFINITY : rows.off[0], total};
+        return;
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;      // (a row that saw nothing is 0)
+    if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - rows.off[0]);
+    T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
+    for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) o[n][dt][v] *= inv;
-            if constexpr (BF) {
-                // lane (i, h) holds columns 8 g + 4 h .. + 3 of its row: the pair exchanges so that each lane stores 16 bytes
+        for (int v = 0; v < 16; ++v) o[dt][v] *= inv;
+        // lane (i, h) holds columns 8 g + 4 h .. + 3 of its row: the pair exchanges so that each lane stores 16 bytes
 #pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    const uint32_t a0 = f2bf_pk(o[n][dt][4 * g], o[n][dt][4 * g + 1]), a1 = f2bf_pk(o[n][dt][4 * g + 2], o[n][dt][4 * g + 3]);
-                    const uint32_t b0 = f2bf_pk(o[n][dt][4 * g + 4], o[n][dt][4 * g + 5]), b1 = f2bf_pk(o[n][dt][4 * g + 6], o[n][dt][4 * g + 7]);
-                    const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
-                    const auto s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-                    const int col = 32 * dt + 8 * (g + lh);
-                    if (ok && col < a.d) *(uint4*)(out + col) = uint4{s0[0], s1[0], s0[1], s1[1]};
-                }
-            } else {
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int col = 32 * dt + 8 * g + 4 * lh;
-                    if (ok && col < a.d) *(float4*)(out + col) = float4{o[n][dt][4 * g], o[n][dt][4 * g + 1], o[n][dt][4 * g + 2], o[n][dt][4 * g + 3]};
-                }
-            }
+        for (int g = 0; g < 4; g += 2) {
+            const uint32_t a0 = f2bf_pk(o[dt][4 * g], o[dt][4 * g + 1]), a1 = f2bf_pk(o[dt][4 * g + 2], o[dt][4 * g + 3]);
+            const uint32_t b0 = f2bf_pk(o[dt][4 * g + 4], o[dt][4 * g + 5]), b1 = f2bf_pk(o[dt][4 * g + 6], o[dt][4 * g + 7]);
+            const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            const int col = 32 * dt + 8 * (g + lh);
+            if (ok && col < a.d) *(uint4*)(out + col) = uint4{s0[0], s1[0], s0[1], s1[1]};
         }
     }
 }
 
+// Few rows, and float tensors of any length: a workgroup has 32 rows, and its wavefronts divide the keys, every W-th 32 of them
+// each, in LDS of their own without a barrier, and join their rows at the end.  A float step's products (32 x 32 x 2, 64 cycles)
+// take long enough that nothing else counts; for bf16 it is the form that spreads little work over the chip.
+template <typename T, int DT> constexpr int prompt_split_tile() { return 2 * 32 * 32 * DT * (int)sizeof(T); }      // K and V, 32 keys
+template <typename T, int DT> constexpr int prompt_split_waves() { return 4 * prompt_split_tile<T, DT>() <= 128 * 1024 ? 4 : 2; }
+// staging, or the joining rows (float), and per column three keys, a word, per wavefront and row an offset and a sum
+template <typename T, int DT> constexpr int prompt_split_lds() {
+    return prompt_split_waves<T, DT>() * prompt_split_tile<T, DT>() + 32 * DT * 12 + 16 + 4 * 32 * 8;
+}
+template <typename T, int DT>
+__global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_split_kernel(PromptArgs a) {
+    typedef PromptRows<T, DT, 1, 1> Rows;
+    constexpr int C = Rows::C, D = Rows::D, KEYS = 32, W = prompt_split_waves<T, DT>(), THREADS = 64 * W;
+    typedef PromptKeys<T, C, KEYS, 64> Keys;
+    static_assert(2 * Keys::TILE == prompt_split_tile<T, DT>() && 32 * D * 4 <= 2 * Keys::TILE, "a wavefront's rows fit its staging");
+    extern __shared__ uint4 lds[];
+    OddColumn* const oddc = (OddColumn*)(lds + W * 2 * KEYS * C);
+    int* const any_odd = (int*)(oddc + D);
+    float2* const ml = (float2*)(any_odd + 4);
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const PromptPlace<32> at(a);
+    if (at.r_base >= at.rows) return;
+    int t0, t1;
+    at.steps<KEYS>(a.shares, &t0, &t1);
+    const Keys keys(a, at.k_first, at.nk, at.hk, lane);
+    uint4* const own = lds + wave * 2 * KEYS * C;
+    const uint32_t sk = (uint32_t)(uintptr_t)(lds_ptr_t)own;
+    if (t0 + wave < t1) keys.load(t0 + wave, sk, 0, lane);
+    if (keys.dc < C) keys.clear(own, 2, lane);
+    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
+    if (tid == 0) *any_odd = 0;
+    Rows rows;
+    rows.init(a, at.q_first, at.hk, at.r_base, at.rows, lane, [&](int r) { return at.limit(r); });
+    __syncthreads();                                 // (the columns' odd values are set up)
+    for (int t = t0 + wave; t < t1; t += W) {
+        wait_staged();
+        const bool masked = (t + 1) * KEYS > at.lo;
+        if (masked) keys.look_over(t, own + KEYS * C, lane, oddc, any_odd);
+        __builtin_amdgcn_wave_barrier();
+        rows.step(sk, sk + Keys::TILE, t * KEYS, masked, a.sl, lane);
+        __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0): the tile has been read
+        __builtin_amdgcn_wave_barrier();
+        if (t + W < t1) keys.load(t + W, sk, 0, lane);
+    }
+    // the wavefronts' parts of a row, brought to the smallest offset
+    const float sum = pair_sum(rows.sum[0]);
+    if (lh == 0) ml[wave * 32 + li] = float2{sum == 0.f ? INFINITY : rows.off[0], sum};
+    __syncthreads();                                 // (staging is free, odd values are noted)
+    float* const joint = (float*)lds;
+    {
+        float off = INFINITY;
+#pragma unroll
+        for (int w = 0; w < W; ++w) off = fminf(off, ml[w * 32 + li].x);
+        const float f = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(off - rows.off[0]);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x16& o = rows.o[0][dt];
+                *(float4*)(joint + (wave * 32 + li) * D + ((32 * dt + 8 * g + 4 * lh) ^ (4 * (li & 7)))) =
+                    float4{f * o[4 * g], f * o[4 * g + 1], f * o[4 * g + 2], f * o[4 * g + 3]};
+            }
+    }
+    __syncthreads();
+    const int n = at.r_end - at.r_base, dq = a.d / 4;
+    const bool odd = *any_odd != 0;
+    for (int q = tid; q < n * dq; q += THREADS) {
+        const int i = q / dq, c = q % dq * 4, r = at.r_base + i, head = at.hk * a.G + r % a.G;
+        const long long row = at.q_first + r / a.G;
+        float off = INFINITY, total = 0.f;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) off = fminf(off, ml[w * 32 + i].x);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float2 y = ml[w * 32 + i];
+            if (y.y != 0.f) total += __builtin_amdgcn_exp2f(off - y.x) * y.y;
+            const float4 z = *(const float4*)(joint + (w * 32 + i) * D + (c ^ (4 * (i & 7))));
+            x[0] += z.x; x[1] += z.y; x[2] += z.z; x[3] += z.w;
+        }
+        if (odd) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = with_odd(x[e], oddc[c + e], at.limit(r));
+        }
+        if (a.shares > 1) {
+            const long long all = (long long)a.n_q * a.Hq, p0 = (long long)at.share * all + row * a.Hq + head;
+            *(float4*)(a.part + p0 * a.d + c) = float4{x[0], x[1], x[2], x[3]};
+            if (c == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[p0] = float2{total == 0.f ? INFINITY : off, total};
+            continue;
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        if (a.lse && c == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off);
+        T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head + c;
+        if constexpr (Rows::BF) *(uint2*)out = uint2{f2bf_pk(x[0] * inv, x[1] * inv), f2bf_pk(x[2] * inv, x[3] * inv)};
+        else *(float4*)out = float4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    }
+}
+
 // Shares of a row's keys -> the row: offsets brought to the smallest, outputs and sums added, a workgroup's wavefronts every fourth
-// share each and then in order.  One workgroup per row.
+// share each and then in order.  One workgroup per row of many shares.
 struct JoinArgs {
     const float* part;             // [shares][n_q Hq][d], then [shares][n_q Hq][2]: offset (+inf: nothing seen), sum
     void* O;
@@ -466,10 +616,53 @@ __device__ __forceinline__ void join_row(const JoinArgs& a, int b, int r) {
     if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(o.x * inv, o.y * inv), f2bf_pk(o.z * inv, o.w * inv)};
     else *(float4*)out = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
 }
+// ... of few shares: one wavefront per row.
+constexpr int kJoinFew = 8;
 template <typename T>
-__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) {
-    const int per = a.max_q * a.Hq;
-    join_row<T>(a, blockIdx.x / per, blockIdx.x % per);
+__device__ __forceinline__ void join_row_few(const JoinArgs& a, int b, int r) {
+    const int lane = threadIdx.x & 63;
+    const PackedSpan qs(a.q_off, b, a.n_q);
+    const int tok = r / a.Hq, head = r % a.Hq;
+    if (tok >= (qs.count < a.max_q ? qs.count : a.max_q)) return;
+    const int shares = shares_of(a.lengths, b, a.share_keys, a.max_len, a.shares);
+    const long long row = qs.first + tok, all = (long long)a.n_q * a.Hq, at = row * a.Hq + head;
+    const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d) + at;
+    const bool cols = 4 * lane < a.d;
+    const float* const p = a.part + at * a.d + 4 * lane;
+    float4 x[kJoinFew];
+    float2 y[kJoinFew];
+    float off = INFINITY, total = 0.f;
+#pragma unroll
+    for (int s = 0; s < kJoinFew; ++s) {
+        y[s] = s < shares ? ml[(long long)s * all] : float2{INFINITY, 0.f};
+        x[s] = s < shares && cols ? *(const float4*)(p + (long long)s * all * a.d) : float4{0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int s = 0; s < kJoinFew; ++s) off = fminf(off, y[s].x);
+    float4 o = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kJoinFew; ++s) {
+        if (y[s].x == INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(off - y[s].x);      // (an offset that is NaN stays one)
+        total += f * y[s].y;
+        o.x += f * x[s].x; o.y += f * x[s].y; o.z += f * x[s].z; o.w += f * x[s].w;
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    if (a.lse && lane == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - off);
+    if (!cols) return;
+    T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head + 4 * lane;
+    if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(o.x * inv, o.y * inv), f2bf_pk(o.z * inv, o.w * inv)};
+    else *(float4*)out = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
 }
+// the workgroups that all rows need, and which a workgroup has
+__host__ __device__ inline int join_blocks_per_sequence(int max_q, int Hq, int shares) { return shares <= kJoinFew ? (max_q * Hq + 3) / 4 : max_q * Hq; }
+template <typename T>
+__device__ __forceinline__ void join_block(const JoinArgs& a, int block) {
+    const int per = join_blocks_per_sequence(a.max_q, a.Hq, a.shares), b = block / per, r = block % per;
+    if (a.shares <= kJoinFew) join_row_few<T>(a, b, 4 * r + (threadIdx.x >> 6));
+    else join_row<T>(a, b, r);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) { join_block<T>(a, blockIdx.x); }
 
 }  // namespace csat

@@ -33,7 +33,7 @@ hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st
 }
 
 hipError_t cache_join_launch(bool bf16, const JoinArgs& j, const CachedArgs& a, hipStream_t st) {
-    const long long o_blocks = (long long)a.B * a.max_q * a.Hq, w_blocks = a.scores ? (long long)a.B * a.Hkv * ((a.c.max_len + 1023) / 1024) : 0;
+    const long long o_blocks = (long long)a.B * join_blocks_per_sequence(a.max_q, a.Hq, a.shares), w_blocks = a.scores ? (long long)a.B * a.Hkv * ((a.c.max_len + 1023) / 1024) : 0;
     const dim3 grid((unsigned)(o_blocks + w_blocks));
     if (bf16) hipLaunchKernelGGL(cache_join_kernel<bf16_t>, grid, dim3(256), 0, st, j, a, (int)o_blocks);
     else hipLaunchKernelGGL(cache_join_kernel<float>, grid, dim3(256), 0, st, j, a, (int)o_blocks);

@@ -16,16 +16,21 @@ typedef float T;
 #define CSAT_TU_FN(name) name##_f32
 #endif
 
-hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, hipStream_t st) {
-    auto launch = [&](auto kernel, int lds_bytes) -> hipError_t {
+hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, bool split, hipStream_t st) {
+    auto launch = [&](auto kernel, int threads, int lds_bytes) -> hipError_t {
         if (lds_bytes > 64 * 1024) {
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.B * a.Hkv * a.tiles * a.shares)), dim3(64 * kPromptWaves), lds_bytes, st, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.B * a.Hkv * a.tiles * a.shares)), dim3(threads), lds_bytes, st, a);
         return hipGetLastError();
     };
-#define CSAT_PROMPT(DT_) launch(prompt_kernel<T, DT_, 1>, prompt_lds_bytes<T, DT_>())
+#if CSAT_TU_BF16
+#define CSAT_PROMPT(DT_) (split ? launch(prompt_split_kernel<T, DT_>, 64 * prompt_split_waves<T, DT_>(), prompt_split_lds<T, DT_>()) \
+                                : launch(prompt_kernel<DT_>, 64 * kPromptWaves, prompt_lds<DT_>()))
+#else
+#define CSAT_PROMPT(DT_) launch(prompt_split_kernel<T, DT_>, 64 * prompt_split_waves<T, DT_>(), prompt_split_lds<T, DT_>())
+#endif
     if (a.d <= 64) return CSAT_PROMPT(2);
     if (a.d <= 96) return CSAT_PROMPT(3);
     if (a.d <= 128) return CSAT_PROMPT(4);
@@ -34,7 +39,7 @@ hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, hipStream_t st) {
 }
 
 hipError_t CSAT_TU_FN(attention_join_launch)(const JoinArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((long long)a.B * a.max_q * a.Hq)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((long long)a.B * join_blocks_per_sequence(a.max_q, a.Hq, a.shares))), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

@@ -11,6 +11,7 @@
 // and the scores' accumulator layout is the B operand of the second product (K-slot order 4h + {0..3}, 8 + 4h + {0..3}
 // in lane half h; V^T comes from the transposing LDS load in the same order).
 #pragma once
+#include "csat_gemm_f32.h"      // split3
 #include "csat_kernels.h"
 
 namespace csat {
@@ -107,41 +108,80 @@ template <typename T, int C> __device__ __forceinline__ int swizzle_v(int row) {
     return C % 16 == 0 ? 4 * (row & 3) : C % 8 == 0 ? 4 * ((row >> 1) & 1) : 0;
 }
 
-// What a wavefront keeps of NT x 32 rows and does with KT x 32 keys in LDS.
-template <typename T, int DT, int NT, int KT>
-struct PromptRows {
+// What a wavefront accumulates for 32 rows, and what becomes of a tile's scores.
+template <int DT>
+struct PromptAcc {
+    f32x16 o[DT];
+    float ref, off, sum;                  // reference score, what a weight's exponent takes off for it, this lane's share of the row's sum
+    int lim;                              // keys that the lane's row sees
+    __device__ __forceinline__ void clear() {
+        ref = -INFINITY; off = 0.f; sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[t][v] = 0.f;
+    }
+    // scores of KT x 32 keys from key0 on -> weights, what was accumulated brought to their reference
+    template <int KT>
+    __device__ __forceinline__ void weights(f32x16 (&s)[KT], int key0, bool masked, float sl, int lh) {
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (key0 + 32 * u + 8 * (v >> 2) + 4 * lh + (v & 3) >= lim) s[u][v] = -INFINITY;
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int u = 0; u < KT; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[u][v]);
+        mx = pair_max(mx);
+        if (__builtin_amdgcn_ballot_w64((mx - ref) * sl > 8.f) != 0) {      // (both lanes of a pair agree; -inf against -inf is no)
+            // before a row's first score there is nothing to rescale, and no offset that means anything
+            const float nm = fmaxf(mx, ref), to = nm == -INFINITY ? 0.f : -nm * sl;
+            const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off);
+            ref = nm;
+            off = to;
+            sum *= f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[dt][v] *= f;
+        }
+#pragma unroll
+        for (int u = 0; u < KT; ++u)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][v], sl, off));
+                sum += s[u][v];
+            }
+    }
+};
+
+// 32 rows against KT x 32 keys in LDS, on the matrix instruction of the tensors' type.
+template <typename T, int DT, int KT>
+struct PromptRows : PromptAcc<DT> {
+    using PromptAcc<DT>::o;
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr int D = 32 * DT, EPC = Elem<T>::per_chunk, C = D / EPC, NK = C / 2;      // 16-byte pieces of a row, pairs of them
-    uint4 qf[NT][NK];
-    f32x16 o[NT][DT];
-    float ref[NT], off[NT], sum[NT];      // reference score, what a weight's exponent takes off for it, this lane's share of the row's sum
-    int lim[NT];                          // keys that the lane's row sees
+    uint4 qf[NK];
 
-    // rows base .. of `rows` (beyond them the last one)
-    template <typename Limit>
-    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int base, int rows, int lane, Limit limit_of) {
-        const int li = lane & 31, lh = lane >> 5, dc = a.d / EPC;
+    // row r of key head hk's rows
+    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, int lane) {
+        const int lh = lane >> 5, dc = a.d / EPC;
+        this->clear();
+        this->lim = limit;
+        const T* q = (const T*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
+        if (dc == C) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            int r = base + 32 * n + li;
-            if (r >= rows) r = rows - 1;
-            lim[n] = limit_of(r);
-            const T* q = (const T*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
-            if (dc == C) {
+            for (int g = 0; g < NK; ++g) qf[g] = *(const uint4*)(q + (2 * g + lh) * EPC);
+        } else {
 #pragma unroll
-                for (int g = 0; g < NK; ++g) qf[n][g] = *(const uint4*)(q + (2 * g + lh) * EPC);
-            } else {
-#pragma unroll
-                for (int g = 0; g < NK; ++g) {
-                    const int c = 2 * g + lh;
-                    qf[n][g] = c < dc ? *(const uint4*)(q + c * EPC) : uint4{0u, 0u, 0u, 0u};
-                }
+            for (int g = 0; g < NK; ++g) {
+                const int c = 2 * g + lh;
+                qf[g] = c < dc ? *(const uint4*)(q + c * EPC) : uint4{0u, 0u, 0u, 0u};
             }
-            ref[n] = -INFINITY; off[n] = 0.f; sum[n] = 0.f;
-#pragma unroll
-            for (int t = 0; t < DT; ++t)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[n][t][v] = 0.f;
         }
     }
 
@@ -152,58 +192,19 @@ struct PromptRows {
         typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
         typedef __attribute__((address_space(3))) const float* lds_float;
         const int li = lane & 31, lh = lane >> 5;
-        f32x16 s[NT][KT];
+        f32x16 s[KT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int u = 0; u < KT; ++u)
 #pragma unroll
-            for (int u = 0; u < KT; ++u)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[n][u][v] = 0.f;
+            for (int v = 0; v < 16; ++v) s[u][v] = 0.f;
 #pragma unroll
         for (int g = 0; g < NK; ++g)
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
                 const u32x4 kf = *(lds_u32x4)(uintptr_t)(sk + (uint32_t)(((32 * u + li) * C + ((2 * g + lh) ^ swizzle_k<C>(li))) * 16));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mfma_group<T>(__builtin_bit_cast(uint4, kf), qf[n][g], s[n][u]);
+                mfma_group<T>(__builtin_bit_cast(uint4, kf), qf[g], s[u]);
             }
-        if (masked) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int u = 0; u < KT; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if (key0 + 32 * u + 8 * (v >> 2) + 4 * lh + (v & 3) >= lim[n]) s[n][u][v] = -INFINITY;
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float mx = s[n][0][0];
-#pragma unroll
-            for (int u = 0; u < KT; ++u)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[n][u][v]);
-            mx = pair_max(mx);
-            if (__builtin_amdgcn_ballot_w64((mx - ref[n]) * sl > 8.f) != 0) {      // (both lanes of a pair agree; -inf against -inf is no)
-                // before a row's first score there is nothing to rescale, and no offset that means anything
-                const float nm = fmaxf(mx, ref[n]), to = nm == -INFINITY ? 0.f : -nm * sl;
-                const float f = ref[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off[n]);
-                ref[n] = nm;
-                off[n] = to;
-                sum[n] *= f;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) o[n][dt][v] *= f;
-            }
-#pragma unroll
-            for (int u = 0; u < KT; ++u)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    s[n][u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][u][v], sl, off[n]));
-                    sum[n] += s[n][u][v];
-                }
-        }
+        this->template weights<KT>(s, key0, masked, sl, lh);
         // O^T += V^T P^T
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
@@ -211,13 +212,9 @@ struct PromptRows {
                 const int l = lane & 15;
 #pragma unroll
                 for (int h2 = 0; h2 < 2; ++h2) {
-                    uint4 pf[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const f32x16& e = s[n][u];
-                        pf[n] = uint4{f2bf_pk(e[8 * h2], e[8 * h2 + 1]), f2bf_pk(e[8 * h2 + 2], e[8 * h2 + 3]),
-                                      f2bf_pk(e[8 * h2 + 4], e[8 * h2 + 5]), f2bf_pk(e[8 * h2 + 6], e[8 * h2 + 7])};
-                    }
+                    const f32x16& e = s[u];
+                    const uint4 pf = uint4{f2bf_pk(e[8 * h2], e[8 * h2 + 1]), f2bf_pk(e[8 * h2 + 2], e[8 * h2 + 3]),
+                                           f2bf_pk(e[8 * h2 + 4], e[8 * h2 + 5]), f2bf_pk(e[8 * h2 + 6], e[8 * h2 + 7])};
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) {
                         // rows 32 u + 16 h2 + 4 lh + {0..3} and the same + 8, columns 32 dt + 16 (lane / 16 % 2) + {0..15}
@@ -226,8 +223,7 @@ struct PromptRows {
                         const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at0 + (32 * u + 16 * h2) * C * 16));
                         const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)(at0 + (32 * u + 16 * h2 + 8) * C * 16));
                         const uint2 w0 = __builtin_bit_cast(uint2, v0), w1 = __builtin_bit_cast(uint2, v1);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) mfma_group<T>(uint4{w0.x, w0.y, w1.x, w1.y}, pf[n], o[n][dt]);
+                        mfma_group<T>(uint4{w0.x, w0.y, w1.x, w1.y}, pf, o[dt]);
                     }
                 }
             } else {
@@ -238,13 +234,101 @@ struct PromptRows {
                         const int row = 4 * lh + (v & 3), c = 8 * dt + (li >> 2);
                         const uint32_t at = sv + (uint32_t)((row * C + (c ^ swizzle_v<T, C>(row))) * 16 + (li & 3) * 4);
                         const float x = *(lds_float)(uintptr_t)(at + (32 * u + 8 * (v >> 2)) * C * 16);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) o[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[n][u][v], o[n][dt], 0, 0, 0);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[u][v], o[dt], 0, 0, 0);
                     }
             }
         }
     }
 };
+
+// ... float rows on the bf16 instruction: six products of the operands' three parts (csat_gemm_f32.h) in 6/16 of the float
+// instruction's time.  Infinities, and values below 2^-109, whose parts do not say what they are, show in what is accumulated
+// (not finite, or not zero and below 2^-90): the workgroup then starts again with the float instruction.
+template <int DT>
+struct PromptRowsParts : PromptAcc<DT> {
+    using PromptAcc<DT>::o;
+    static constexpr int D = 32 * DT, C = D / 4, NB = D / 16;
+    uint4 qp[NB][3];
+    __device__ __forceinline__ static void parts(const float (&x)[8], uint4 (&p)[3]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split3(x[2 * i], x[2 * i + 1], (&p[0].x)[i], (&p[1].x)[i], (&p[2].x)[i]);
+    }
+    __device__ __forceinline__ static void products(const uint4 (&x)[3], const uint4 (&y)[3], f32x16& acc) {      // small ones first
+        mfma_group<bf16_t>(x[1], y[1], acc);
+        mfma_group<bf16_t>(x[0], y[2], acc);
+        mfma_group<bf16_t>(x[2], y[0], acc);
+        mfma_group<bf16_t>(x[0], y[1], acc);
+        mfma_group<bf16_t>(x[1], y[0], acc);
+        mfma_group<bf16_t>(x[0], y[0], acc);
+    }
+    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, int lane) {
+        const int lh = lane >> 5;
+        this->clear();
+        this->lim = limit;
+        const float* q = (const float*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
+#pragma unroll
+        for (int g = 0; g < NB; ++g) {
+            const int f = 16 * g + 8 * lh;
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (f < a.d) {
+                const float4 x0 = *(const float4*)(q + f), x1 = *(const float4*)(q + f + 4);
+                x[0] = x0.x; x[1] = x0.y; x[2] = x0.z; x[3] = x0.w; x[4] = x1.x; x[5] = x1.y; x[6] = x1.z; x[7] = x1.w;
+            }
+            parts(x, qp[g]);
+        }
+    }
+    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane) {
+        typedef __attribute__((address_space(3))) const f32x4* lds_f32x4;
+        typedef __attribute__((address_space(3))) const float* lds_float;
+        const int li = lane & 31, lh = lane >> 5;
+        f32x16 s[1];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[0][v] = 0.f;
+#pragma unroll
+        for (int g = 0; g < NB; ++g) {
+            float x[8];
+            uint4 kp[3];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 w = *(lds_f32x4)(uintptr_t)(sk + (uint32_t)((li * C + ((4 * g + 2 * lh + h) ^ swizzle_k<C>(li))) * 16));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[4 * h + e] = w[e];
+            }
+            parts(x, kp);
+            products(kp, qp[g], s[0]);
+        }
+        this->template weights<1>(s, key0, masked, sl, lh);
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+            float x[8];
+            uint4 pp[3], vp[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[0][8 * h2 + e];
+            parts(x, pp);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int row = 4 * lh + (e & 3), c = 8 * dt + (li >> 2);
+                    const uint32_t at = sv + (uint32_t)((row * C + (c ^ swizzle_v<float, C>(row))) * 16 + (li & 3) * 4);
+                    x[e] = *(lds_float)(uintptr_t)(at + (16 * h2 + 8 * (e >> 2)) * C * 16);
+                }
+                parts(x, vp);
+                products(vp, pp, o[dt]);
+            }
+        }
+    }
+};
+template <int DT>
+__device__ __forceinline__ bool suspect(const PromptAcc<DT>& a) {
+    SplitSuspect t;
+    t.add(a.sum);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) t.add(a.o[dt][v]);
+    return t.any();
+}
 
 // A sequence's keys in steps of KEYS: a step's pieces go from memory straight into LDS, piece q of the tile at its place there;
 // thread `tid` of THREADS brings the pieces q = THREADS p + tid from the places that the swizzles send there (token strides are
@@ -354,7 +438,7 @@ struct PromptPlace {
 template <int DT>
 __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
     typedef bf16_t T;
-    typedef PromptRows<T, DT, 1, 2> Rows;
+    typedef PromptRows<T, DT, 2> Rows;
     constexpr int C = Rows::C, D = Rows::D, KEYS = 64, THREADS = 64 * kPromptWaves;
     typedef PromptKeys<T, C, KEYS, THREADS> Keys;
     extern __shared__ uint4 lds[];                  // K tile, V tile; the same once more; then the columns' odd values
@@ -377,7 +461,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
     if (tid == 0) *any_odd = 0;
     Rows rows;
-    rows.init(a, at.q_first, at.hk, w_base, at.rows, lane, [&](int r) { return at.limit(r); });
+    const bool ok = w_base + li < at.rows;
+    const int r = ok ? w_base + li : at.rows - 1;
+    rows.init(a, at.q_first, at.hk, r, at.limit(r), lane);
     for (int t = t0; t < t1; ++t) {
         const uint32_t sk = lds0 + (t & 1) * 2 * Keys::TILE;
         wait_staged();
@@ -393,16 +479,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     __syncthreads();                                 // (the last steps' odd values are noted)
     if (!active) return;
 
-    const float total = pair_sum(rows.sum[0]);
-    const bool ok = w_base + li < at.rows;
-    const int r = ok ? w_base + li : at.rows - 1, head = at.hk * a.G + r % a.G;
+    const float total = pair_sum(rows.sum);
+    const int head = at.hk * a.G + r % a.G;
     const long long row = at.q_first + r / a.G;
-    f32x16 (&o)[DT] = rows.o[0];
+    f32x16 (&o)[DT] = rows.o;
     if (*any_odd) {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) o[dt][v] = with_odd(o[dt][v], oddc[32 * dt + 8 * (v >> 2) + 4 * lh + (v & 3)], rows.lim[0]);
+            for (int v = 0; v < 16; ++v) o[dt][v] = with_odd(o[dt][v], oddc[32 * dt + 8 * (v >> 2) + 4 * lh + (v & 3)], rows.lim);
     }
     if (a.shares > 1) {
         const long long all = (long long)a.n_q * a.Hq, p0 = (long long)at.share * all + row * a.Hq + head;
@@ -415,11 +500,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
                 const int col = 32 * dt + 8 * g + 4 * lh;
                 if (col < a.d) *(float4*)(p + col) = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
             }
-        if (lh == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[p0] = float2{total == 0.f ? INFINITY : rows.off[0], total};
+        if (lh == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[p0] = float2{total == 0.f ? INFINITY : rows.off, total};
         return;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;      // (a row that saw nothing is 0)
-    if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - rows.off[0]);
+    if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - rows.off);
     T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -439,8 +524,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
 }
 
 // Few rows, and float tensors of any length: a workgroup has 32 rows, and its wavefronts divide the keys, every W-th 32 of them
-// each, in LDS of their own without a barrier, and join their rows at the end.  A float step's products (32 x 32 x 2, 64 cycles)
-// take long enough that nothing else counts; for bf16 it is the form that spreads little work over the chip.
+// each, in LDS of their own without a barrier, and join their rows at the end.  Float is bound by what a step issues (d 64: 48
+// products of 32 cycles, 570 vector instructions, most of them splitting K, V and the weights); for bf16 it is the form
+// that spreads little work over the chip.
 template <typename T, int DT> constexpr int prompt_split_tile() { return 2 * 32 * 32 * DT * (int)sizeof(T); }      // K and V, 32 keys
 template <typename T, int DT> constexpr int prompt_split_waves() { return 4 * prompt_split_tile<T, DT>() <= 128 * 1024 ? 4 : 2; }
 // staging, or the joining rows (float), and per column three keys, a word, per wavefront and row an offset and a sum
@@ -449,7 +535,7 @@ template <typename T, int DT> constexpr int prompt_split_lds() {
 }
 template <typename T, int DT>
 __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_split_kernel(PromptArgs a) {
-    typedef PromptRows<T, DT, 1, 1> Rows;
+    typedef PromptRows<T, DT, 1> Rows;
     constexpr int C = Rows::C, D = Rows::D, KEYS = 32, W = prompt_split_waves<T, DT>(), THREADS = 64 * W;
     typedef PromptKeys<T, C, KEYS, 64> Keys;
     static_assert(2 * Keys::TILE == prompt_split_tile<T, DT>() && 32 * D * 4 <= 2 * Keys::TILE, "a wavefront's rows fit its staging");
@@ -466,38 +552,48 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
     const Keys keys(a, at.k_first, at.nk, at.hk, lane);
     uint4* const own = lds + wave * 2 * KEYS * C;
     const uint32_t sk = (uint32_t)(uintptr_t)(lds_ptr_t)own;
-    if (t0 + wave < t1) keys.load(t0 + wave, sk, 0, lane);
     if (keys.dc < C) keys.clear(own, 2, lane);
     for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
     if (tid == 0) *any_odd = 0;
-    Rows rows;
-    rows.init(a, at.q_first, at.hk, at.r_base, at.rows, lane, [&](int r) { return at.limit(r); });
-    __syncthreads();                                 // (the columns' odd values are set up)
-    for (int t = t0 + wave; t < t1; t += W) {
-        wait_staged();
-        const bool masked = (t + 1) * KEYS > at.lo;
-        if (masked) keys.look_over(t, own + KEYS * C, lane, oddc, any_odd);
-        __builtin_amdgcn_wave_barrier();
-        rows.step(sk, sk + Keys::TILE, t * KEYS, masked, a.sl, lane);
-        __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0): the tile has been read
-        __builtin_amdgcn_wave_barrier();
-        if (t + W < t1) keys.load(t + W, sk, 0, lane);
+    const int lane_row = at.r_base + li < at.rows ? at.r_base + li : at.rows - 1, lane_limit = at.limit(lane_row);
+    PromptAcc<DT> acc;
+    auto go = [&](auto rows) {
+        if (t0 + wave < t1) keys.load(t0 + wave, sk, 0, lane);
+        rows.init(a, at.q_first, at.hk, lane_row, lane_limit, lane);
+        __syncthreads();                             // (the columns' odd values are set up)
+        for (int t = t0 + wave; t < t1; t += W) {
+            wait_staged();
+            const bool masked = (t + 1) * KEYS > at.lo;
+            if (masked) keys.look_over(t, own + KEYS * C, lane, oddc, any_odd);
+            __builtin_amdgcn_wave_barrier();
+            rows.step(sk, sk + Keys::TILE, t * KEYS, masked, a.sl, lane);
+            __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the tile has been read
+            __builtin_amdgcn_wave_barrier();
+            if (t + W < t1) keys.load(t + W, sk, 0, lane);
+        }
+        acc = rows;
+    };
+    if constexpr (Rows::BF || DT > 4) {              // (256 features in three parts do not fit the registers)
+        go(Rows{});
+    } else {
+        go(PromptRowsParts<DT>{});
+        if (__syncthreads_or(suspect(acc))) go(Rows{});
     }
     // the wavefronts' parts of a row, brought to the smallest offset
-    const float sum = pair_sum(rows.sum[0]);
-    if (lh == 0) ml[wave * 32 + li] = float2{sum == 0.f ? INFINITY : rows.off[0], sum};
+    const float sum = pair_sum(acc.sum);
+    if (lh == 0) ml[wave * 32 + li] = float2{sum == 0.f ? INFINITY : acc.off, sum};
     __syncthreads();                                 // (staging is free, odd values are noted)
     float* const joint = (float*)lds;
     {
         float off = INFINITY;
 #pragma unroll
         for (int w = 0; w < W; ++w) off = fminf(off, ml[w * 32 + li].x);
-        const float f = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(off - rows.off[0]);
+        const float f = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(off - acc.off);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x16& o = rows.o[0][dt];
+                const f32x16& o = acc.o[dt];
                 *(float4*)(joint + (wave * 32 + li) * D + ((32 * dt + 8 * g + 4 * lh) ^ (4 * (li & 7)))) =
                     float4{f * o[4 * g], f * o[4 * g + 1], f * o[4 * g + 2], f * o[4 * g + 3]};
             }

@@ -566,17 +566,30 @@ struct EvictArgs {
 };
 
 constexpr int kSelectThreads = 1024;
-// Which tokens of a sequence and head stay: the least key that does, digit by digit from the highest (counts in LDS), then
-// one pass in slot order.  A key is a weight's bits in an order of whole numbers (NaN highest, -0 as 0).
+// A key is a weight's bits in an order of whole numbers (NaN highest, -0 as 0).
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 0xffffffffu;
     const uint32_t u = __float_as_uint(w + 0.f);
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
+// Inclusive prefix sums over a wavefront.
+__device__ __forceinline__ int wave_prefix(int x, int lane) {
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+        const int y = __shfl_up(x, s);
+        if (lane >= s) x += y;
+    }
+    return x;
+}
+// Which tokens of a sequence and head stay, one workgroup each: the least key that does, digit by digit from the highest (11, 11 and
+// 10 bits, counted in LDS), then one pass in slot order.  Keys are held in registers, kSelectKeys per thread, and read again
+// for every digit only where the sequence is longer than that.  Bound by the chain of its steps, about 1 us each.
+constexpr int kSelectKeys = 8;
 static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(EvictArgs a) {
-    constexpr int BINS = 2048, WAVES = kSelectThreads / 64;
+    constexpr int BINS = 2048, WAVES = kSelectThreads / 64, CHUNK = kSelectThreads * kSelectKeys;
     __shared__ int bins[BINS];
-    __shared__ int wsum[WAVES][2];
+    __shared__ int wsum[WAVES];
+    __shared__ int above[kSelectKeys * WAVES], equal[kSelectKeys * WAVES];
     __shared__ int found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
@@ -584,6 +597,18 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
     int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget;
     bool bad = L < 0 || L > a.from.max_len;
     const int keep = bad ? 0 : L < a.budget ? L : a.budget;
+    const float* const w = a.W + ((long long)b * a.Hkv + hk) * a.from.max_pages * page;
+    float* const w_to = a.W_to + ((long long)b * a.Hkv + hk) * a.to.max_pages * page;
+    const int recent = keep < a.recent ? keep : a.recent, n = bad ? 0 : L - recent, k = keep - recent;      // k of the first n
+    float x[kSelectKeys];
+    auto load = [&](int c) {
+#pragma unroll
+        for (int r = 0; r < kSelectKeys; ++r) {
+            const int i = c * CHUNK + r * kSelectThreads + tid;
+            x[r] = i < n ? w[i] : 0.f;
+        }
+    };
+    load(0);
     if (!bad) {
         for (int i = tid; i < (L + page - 1) / page; i += kSelectThreads) {
             const int id = a.from.table[(long long)b * a.from.max_pages + i];
@@ -594,91 +619,91 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
             bad |= id < 0 || id >= a.to.pages;
         }
     }
+    for (int i = tid; i < BINS; i += kSelectThreads) bins[i] = 0;
     bad = __syncthreads_or(bad) != 0;
     if (tid == 0 && hk == 0) a.to.lengths[b] = bad ? -1 : keep;
-    if (bad) {
-        for (int i = tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
-        return;
-    }
-    for (int i = keep + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
-    const float* const w = a.W + ((long long)b * a.Hkv + hk) * a.from.max_pages * page;
-    float* const w_to = a.W_to + ((long long)b * a.Hkv + hk) * a.to.max_pages * page;
-    const int recent = keep < a.recent ? keep : a.recent, n = L - recent, k = keep - recent;      // k of the first n
+    for (int i = (bad ? 0 : keep) + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+    if (bad) return;
     for (int i = tid; i < recent; i += kSelectThreads) {
         kept[k + i] = n + i;
         w_to[k + i] = w[n + i];
     }
-    // the k-th largest key: prefix bits found so far, how many of the keys with that prefix still have to be taken
+    if (k <= 0) return;
+
+    // the k-th largest key: its bits found so far, how many of the keys that have them are still to be taken
+    const int chunks = (n + CHUNK - 1) / CHUNK;
+    const bool all = k >= n;
     uint32_t prefix = 0;
     int need = k;
-    if (k > 0 && k < n) {
+    if (!all) {
         int bits = 0;
         for (int pass = 0; pass < 3; ++pass) {
             const int width = pass < 2 ? 11 : 10, shift = 32 - bits - width;
-            for (int i = tid; i < BINS; i += kSelectThreads) bins[i] = 0;
-            __syncthreads();
-            for (int i = tid; i < n; i += kSelectThreads) {
-                const uint32_t key = weight_key(w[i]);
-                if (bits == 0 || (key >> (32 - bits)) == prefix) atomicAdd(&bins[(key >> shift) & ((1u << width) - 1u)], 1);
+            for (int c = 0; c < chunks; ++c) {
+                if (chunks > 1) load(c);
+#pragma unroll
+                for (int r = 0; r < kSelectKeys; ++r) {
+                    const uint32_t key = weight_key(x[r]);
+                    if (c * CHUNK + r * kSelectThreads + tid < n && (bits == 0 || (key >> (32 - bits)) == prefix)) atomicAdd(&bins[(key >> shift) & ((1u << width) - 1u)], 1);
+                }
             }
             __syncthreads();
-            if (wave == 0) {      // bins from the highest down: a lane sums 32 of them, then the lane that holds the place looks closer
-                const int per = (1 << width) / 64, top = (1 << width) - 1 - lane * per;
-                int mine = 0;
-                for (int i = 0; i < per; ++i) mine += bins[top - i];
-                int before = mine;
-#pragma unroll
-                for (int s = 1; s < 64; s *= 2) {
-                    const int y = __shfl_up(before, s);
-                    if (lane >= s) before += y;
-                }
-                before -= mine;
-                if (before < need && before + mine >= need) {
-                    int left = need - before, i = 0;
-                    while (bins[top - i] < left) { left -= bins[top - i]; ++i; }
-                    found[0] = top - i;
-                    found[1] = left;
-                }
+            // from the highest bin down, two (one) a thread: the thread whose bins hold the place says where it is
+            const int per = (1 << width) / kSelectThreads, top = (1 << width) - 1 - tid * per;
+            const int c0 = bins[top], c1 = per == 2 ? bins[top - 1] : 0, mine = c0 + c1, up_to = wave_prefix(mine, lane);
+            if (lane == 63) wsum[wave] = up_to;
+            __syncthreads();
+            int before = up_to - mine;
+            for (int v = 0; v < wave; ++v) before += wsum[v];
+            bins[top] = 0;
+            if (per == 2) bins[top - 1] = 0;
+            if (before < need && before + mine >= need) {
+                const bool second = before + c0 < need;
+                found[0] = second ? top - 1 : top;
+                found[1] = need - before - (second ? c0 : 0);
             }
             __syncthreads();
             prefix = (prefix << width) | (uint32_t)found[0];
             need = found[1];
             bits += width;
-            __syncthreads();
         }
     }
-    // in slot order: keys above the k-th, and the first `need` of those equal to it.  A wavefront takes a stretch of slots.
-    if (k <= 0) return;
-    const bool all = k >= n;
-    const int stretch = ((n + WAVES - 1) / WAVES + 63) / 64 * 64, s0 = wave * stretch, s1 = s0 + stretch < n ? s0 + stretch : n;
-    int above = 0, equal = 0;
-    for (int i0 = s0; i0 < s1; i0 += 64) {
-        const int i = i0 + lane;
-        const uint32_t key = i < s1 ? weight_key(w[i]) : 0;
-        const bool in = i < s1;
-        above += __popcll(__ballot(in && (all || key > prefix)));
-        equal += __popcll(__ballot(in && !all && key == prefix));
-    }
-    if (lane == 0) { wsum[wave][0] = above; wsum[wave][1] = equal; }
-    __syncthreads();
+    // in slot order: keys above the k-th, and the first `need` of those equal to it
     int at_above = 0, at_equal = 0;
-    for (int v = 0; v < wave; ++v) { at_above += wsum[v][0]; at_equal += wsum[v][1]; }
     const unsigned long long below = (1ull << lane) - 1ull;
-    for (int i0 = s0; i0 < s1; i0 += 64) {
-        const int i = i0 + lane;
-        const bool in = i < s1;
-        const float x = in ? w[i] : 0.f;
-        const uint32_t key = weight_key(x);
-        const unsigned long long ma = __ballot(in && (all || key > prefix)), me = __ballot(in && !all && key == prefix);
-        const int ra = at_above + __popcll(ma & below), re = at_equal + __popcll(me & below);
-        const bool is_above = (ma >> lane) & 1, is_equal = (me >> lane) & 1;
-        if (is_above || (is_equal && re < need)) {
-            const int p = ra + (re < need ? re : need);
-            kept[p] = i;
-            w_to[p] = x;
+    for (int c = 0; c < chunks; ++c) {
+        if (chunks > 1) load(c);
+        unsigned long long ma[kSelectKeys], me[kSelectKeys];
+        if (c) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSelectKeys; ++r) {
+            const bool in = c * CHUNK + r * kSelectThreads + tid < n;
+            const uint32_t key = weight_key(x[r]);
+            ma[r] = __ballot(in && (all || key > prefix));
+            me[r] = __ballot(in && !all && key == prefix);
+            if (lane == 0) { above[r * WAVES + wave] = __popcll(ma[r]); equal[r * WAVES + wave] = __popcll(me[r]); }
         }
-        at_above += __popcll(ma);
-        at_equal += __popcll(me);
+        __syncthreads();
+        if (wave < 2) {      // exclusive sums over the kSelectKeys * WAVES = 128 counts
+            int* const p = wave == 0 ? above : equal;
+            const int x0 = p[2 * lane], x1 = p[2 * lane + 1], up_to = wave_prefix(x0 + x1, lane);
+            p[2 * lane] = up_to - x0 - x1;
+            p[2 * lane + 1] = up_to - x1;
+            if (lane == 63) wsum[wave] = up_to;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSelectKeys; ++r) {
+            const int ra = at_above + above[r * WAVES + wave] + __popcll(ma[r] & below), re = at_equal + equal[r * WAVES + wave] + __popcll(me[r] & below);
+            const bool is_above = (ma[r] >> lane) & 1, is_equal = (me[r] >> lane) & 1;
+            if (is_above || (is_equal && re < need)) {
+                const int p = ra + (re < need ? re : need);
+                kept[p] = c * CHUNK + r * kSelectThreads + tid;
+                w_to[p] = x[r];
+            }
+        }
+        at_above += wsum[0];
+        at_equal += wsum[1];
     }
 }
 

@@ -528,10 +528,16 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
 // products of 32 cycles, 570 vector instructions, most of them splitting K, V and the weights); for bf16 it is the form
 // that spreads little work over the chip.
 template <typename T, int DT> constexpr int prompt_split_tile() { return 2 * 32 * 32 * DT * (int)sizeof(T); }      // K and V, 32 keys
-template <typename T, int DT> constexpr int prompt_split_waves() { return 4 * prompt_split_tile<T, DT>() <= 128 * 1024 ? 4 : 2; }
+// bf16: as many wavefronts as the LDS holds tiles for, up to 8, since a row tile's keys are a chain (2 key heads x 1024 x 4, d 128: 13.4
+// against 15.9 us with 4).  Float: 4, so that two workgroups share a CU's vector units and one fills the other's start and
+// end (a clip of 1600 tokens, 12 heads: 40 against 54 us with 8); 2 for 256 features.
+template <typename T, int DT> constexpr int prompt_split_waves() {
+    const int most = sizeof(T) == 2 ? 8 : 4;
+    return most * prompt_split_tile<T, DT>() <= 128 * 1024 ? most : most / 2;
+}
 // staging, or the joining rows (float), and per column three keys, a word, per wavefront and row an offset and a sum
 template <typename T, int DT> constexpr int prompt_split_lds() {
-    return prompt_split_waves<T, DT>() * prompt_split_tile<T, DT>() + 32 * DT * 12 + 16 + 4 * 32 * 8;
+    return prompt_split_waves<T, DT>() * (prompt_split_tile<T, DT>() + 32 * 8) + 32 * DT * 12 + 16;
 }
 template <typename T, int DT>
 __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_split_kernel(PromptArgs a) {

@@ -104,8 +104,21 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     const T* V = (const T*)a.V + row0 * a.v_token + (long long)hk * a.v_head;
     const int dq = a.d / 4, items = page / 4 * dq;
     typedef typename std::conditional<sizeof(T) == 2, uint2, float4>::type Four;
+    // everything that memory has to say is asked for at once: the block's scales and, at the ends of the new tokens, what 16 slots hold
+    const int id = table[j];
+    bool bad = id < 0 || id >= a.c.pages;
+    const long long block = (long long)(bad ? 0 : id) * a.Hkv + hk;
+    const float ok = lo ? a.c.Ks[block] : 0.f, ov = lo ? a.c.Vs[block] : 0.f;
+    uint8_t* const ck = a.c.K + block * page * a.d;
+    uint8_t* const cv = a.c.V + block * page * a.d;
+    const int lg = a.c.log_page - 4, groups = 1 << lg, pieces = a.d << lg;      // 16-token pieces of V's features
+    uint4 was[NI];
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, g = (q & (groups - 1)) * 16;
+        was[p] = q < pieces && g < hi && g + 16 > lo && (g < lo || g + 16 > hi) ? ((const uint4*)cv)[q] : uint4{0u, 0u, 0u, 0u};
+    }
     Four xk[NI][4], xv[NI][4];
-    bool bad = false;
 #pragma unroll
     for (int p = 0; p < NI; ++p) {
         const int q = p * 256 + tid, s = q / dq * 4, f = q % dq * 4;
@@ -143,10 +156,6 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     mv = wave_max(mv);
     if ((tid & 63) == 0) { red[0][tid >> 6] = mk; red[1][tid >> 6] = mv; }
     if (__syncthreads_or(bad)) return;
-    const long long block = (long long)table[j] * a.Hkv + hk;
-    const float ok = lo ? a.c.Ks[block] : 0.f, ov = lo ? a.c.Vs[block] : 0.f;
-    uint8_t* const ck = a.c.K + block * page * a.d;
-    uint8_t* const cv = a.c.V + block * page * a.d;
     mk = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
     mv = fmaxf(fmaxf(red[1][0], red[1][1]), fmaxf(red[1][2], red[1][3]));
     const float sk = fmaxf(pow2f(scale_exponent(mk)), ok), sv = fmaxf(pow2f(scale_exponent(mv)), ov);
@@ -176,27 +185,26 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     }
     __syncthreads();
     if (tid == 0) { a.c.Ks[block] = sk; a.c.Vs[block] = sv; }      // (behind the barrier: every thread has read the old ones)
-    const int groups = page / 16;
     const float fv = ov * iv;
-    for (int q = tid; q < groups * a.d; q += 256) {
-        const int g = q % groups * 16, f = q / groups;
-        if (g >= hi || (g + 16 <= lo && sv == ov)) continue;
-        uint4* const out = (uint4*)(cv + (long long)f * page + g);
+#pragma unroll
+    for (int p = 0; p < NI; ++p) {
+        const int q = p * 256 + tid, g = (q & (groups - 1)) * 16, f = q >> lg;
+        if (q >= pieces || g >= hi || (g + 16 <= lo && sv == ov)) continue;
         uint4 w;
 #pragma unroll
         for (int k = 0; k < 4; ++k) (&w.x)[k] = *(const uint32_t*)((const uint8_t*)turned + f * pitch + g + 4 * k);
         if (g < lo || g + 16 > hi) {
-            const uint4 was = *out;
+            if (g + 16 <= lo) was[p] = ((const uint4*)cv)[q];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int s = g + 4 * k;
                 const uint32_t in = byte_mask(s, lo, hi), old = byte_mask(s, 0, lo);
-                uint32_t x = (&was.x)[k];
+                uint32_t x = (&was[p].x)[k];
                 if (old && sv != ov) x = (rescale_codes(x, fv) & old) | (x & ~old);
                 (&w.x)[k] = ((&w.x)[k] & in) | (x & ~in);
             }
         }
-        *out = w;
+        ((uint4*)cv)[q] = w;
     }
 }
 
@@ -514,19 +522,29 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
     const int shares = shares_of(a.c.lengths, b, a.share_tokens, a.c.max_len, a.shares);
     float* const w = a.W + ((long long)b * a.Hkv + hk) * a.c.max_pages * a.c.page + t;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
+    // four rows' scores are asked for ahead of what they are weighed with
+    const float* const scores = a.scores + ((long long)b * a.Hkv + hk) * a.max_q * a.G * a.score_ld + t;
+    float4 y[4];
+    auto ask = [&](int r) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = r + k < rows && t < L ? *(const float4*)(scores + (long long)(r + k) * a.score_ld) : float4{0.f, 0.f, 0.f, 0.f};
+    };
+    ask(0);
     for (int r0 = 0; r0 < rows; r0 += RB) {
         const int n = rows - r0 < RB ? rows - r0 : RB;
         __syncthreads();
         for (int i = tid >> 6; i < n; i += 4) {      // a wavefront a row
             const int r = r0 + i;
             const long long at = (long long)(qs.first + r / a.G) * a.Hq + hk * a.G + r % a.G;
-            float off = INFINITY, total = 0.f;
-            for (int s = lane; s < shares; s += 64) off = fminf(off, ml[(long long)s * all + at].x);
+            const float2 z = lane < shares ? ml[(long long)lane * all + at] : float2{INFINITY, 0.f};      // (the first 64 shares)
+            float off = z.x;
+            for (int s = lane + 64; s < shares; s += 64) off = fminf(off, ml[(long long)s * all + at].x);
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) off = fminf(off, __shfl_xor(off, s));
-            for (int s = lane; s < shares; s += 64) {
-                const float2 y = ml[(long long)s * all + at];
-                if (y.x != INFINITY) total += __builtin_amdgcn_exp2f(off - y.x) * y.y;
+            float total = z.x == INFINITY ? 0.f : __builtin_amdgcn_exp2f(off - z.x) * z.y;
+            for (int s = lane + 64; s < shares; s += 64) {
+                const float2 v = ml[(long long)s * all + at];
+                if (v.x != INFINITY) total += __builtin_amdgcn_exp2f(off - v.x) * v.y;
             }
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
@@ -537,16 +555,24 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
             }
         }
         __syncthreads();
-        if (t >= L) continue;
-        const float* s = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G + r0) * a.score_ld + t;
-        for (int i = 0; i < n; ++i, s += a.score_ld) {
-            const float4 y = *(const float4*)s;
-            const float l = lse2[i];
-            const int seen = limit[i];
+        for (int i = 0; i < n; i += 4) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (t + e < seen) x[e] += __builtin_amdgcn_exp2f((&y.x)[e] - l);
+            for (int k = 0; k < 4; ++k) {
+                const float l = i + k < n ? lse2[i + k] : INFINITY;
+                const int seen = i + k < n ? limit[i + k] : 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (t + e < seen) x[e] += __builtin_amdgcn_exp2f((&y[k].x)[e] - l);
+            }
+            ask(r0 + i + 4);
         }
+    }
+    if (t >= L) return;
+    if (t + 4 <= L) {
+        float4* const to = (float4*)w;
+        const float4 was = a.decay == 0.f ? float4{0.f, 0.f, 0.f, 0.f} : *to;
+        *to = float4{x[0] + a.decay * was.x, x[1] + a.decay * was.y, x[2] + a.decay * was.z, x[3] + a.decay * was.w};
+        return;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -590,7 +616,7 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
     __shared__ int bins[BINS];
     __shared__ int wsum[WAVES];
     __shared__ int above[kSelectKeys * WAVES], equal[kSelectKeys * WAVES];
-    __shared__ int found[2];
+    __shared__ int found[3];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
     const int L = a.from.lengths[b], page = a.from.page;
@@ -634,7 +660,7 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
     const int chunks = (n + CHUNK - 1) / CHUNK;
     const bool all = k >= n;
     uint32_t prefix = 0;
-    int need = k;
+    int need = k, low = 0;                           // (low: the bits not looked at, where all keys with the others' value are taken)
     if (!all) {
         int bits = 0;
         for (int pass = 0; pass < 3; ++pass) {
@@ -661,11 +687,14 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
                 const bool second = before + c0 < need;
                 found[0] = second ? top - 1 : top;
                 found[1] = need - before - (second ? c0 : 0);
+                found[2] = second ? c1 : c0;
             }
             __syncthreads();
             prefix = (prefix << width) | (uint32_t)found[0];
             need = found[1];
             bits += width;
+            low = 32 - bits;
+            if (need == found[2]) break;
         }
     }
     // in slot order: keys above the k-th, and the first `need` of those equal to it
@@ -678,7 +707,7 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
 #pragma unroll
         for (int r = 0; r < kSelectKeys; ++r) {
             const bool in = c * CHUNK + r * kSelectThreads + tid < n;
-            const uint32_t key = weight_key(x[r]);
+            const uint32_t key = weight_key(x[r]) >> low;
             ma[r] = __ballot(in && (all || key > prefix));
             me[r] = __ballot(in && !all && key == prefix);
             if (lane == 0) { above[r * WAVES + wave] = __popcll(ma[r]); equal[r * WAVES + wave] = __popcll(me[r]); }

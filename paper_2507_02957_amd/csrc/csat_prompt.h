@@ -669,30 +669,32 @@ __device__ __forceinline__ void join_row(const JoinArgs& a, int b, int r) {
     const int shares = shares_of(a.lengths, b, a.share_keys, a.max_len, a.shares);
     const long long row = qs.first + tok, all = (long long)a.n_q * a.Hq, at = row * a.Hq + head;
     const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d) + at;
-    float off = INFINITY, odd = 0.f;
-    for (int s = lane; s < shares; s += 64) {
-        const float x = ml[(long long)s * all].x;
-        off = fminf(off, x);
-        if (x != x) odd = x;
-    }
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-        off = fminf(off, __shfl_xor(off, s));
-        odd += __shfl_xor(odd, s);                   // (0, or NaN)
-    }
     const bool cols = 4 * lane < a.d;
     const float* const p = a.part + at * a.d + 4 * lane;
-    float total = odd;
-    float4 o = float4{odd, odd, odd, odd};           // columns 4 lane .. + 3
-    for (int s0 = wave; s0 < shares; s0 += 4 * kJoinAhead) {
-        float4 x[kJoinAhead];
-        float2 y[kJoinAhead];
+    float4 x[kJoinAhead];                            // a wavefront's next shares: asked for before their weights are known
+    float2 y[kJoinAhead];
+    auto ask = [&](int s0) {
 #pragma unroll
         for (int i = 0; i < kJoinAhead; ++i) {
             const int s = s0 + 4 * i;
             y[i] = s < shares ? ml[(long long)s * all] : float2{INFINITY, 0.f};
             x[i] = s < shares && cols ? *(const float4*)(p + (long long)s * all * a.d) : float4{0.f, 0.f, 0.f, 0.f};
         }
+    };
+    ask(wave);
+    float off = INFINITY, odd = 0.f;
+    for (int s = lane; s < shares; s += 64) {
+        const float v = ml[(long long)s * all].x;
+        off = fminf(off, v);
+        if (v != v) odd = v;
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) off = fminf(off, __shfl_xor(off, s));
+    if (__ballot(odd != odd) != 0) odd = __uint_as_float(0x7fc00000u);
+    float total = odd;
+    float4 o = float4{odd, odd, odd, odd};           // columns 4 lane .. + 3
+    for (int s0 = wave; s0 < shares; s0 += 4 * kJoinAhead) {
+        if (s0 != wave) ask(s0);
 #pragma unroll
         for (int i = 0; i < kJoinAhead; ++i) {
             if (y[i].x == INFINITY) continue;

@@ -2170,7 +2170,9 @@ bool hadamard_fits_lds(int n, int m) {
 
 // ---- Exact attention over packed sequences and the 8-bit cache (csat_prompt.h, csat_cache.h)
 
-constexpr long long kMaxGrid = 0x7fffffffLL;
+constexpr long long kMaxRows = 0x7fffffffLL;
+constexpr long long kMaxBlocks = (1 << 22) - 1;      // workgroups of up to 1024 threads along x ...
+constexpr long long kMaxBlocksYZ = 65535;            // ... and along y and z
 constexpr long long kMaxTokenStride = 1 << 24;
 
 bool stride_ok(long long token, long long head, size_t e) {
@@ -2181,7 +2183,7 @@ csat_status check_packed(const csat_packed_dims* d, int d_multiple) {
     if (d->dtype != CSAT_F32 && d->dtype != CSAT_BF16) return CSAT_ERR_DTYPE;
     if (d->B <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->d <= 0 || d->n_q <= 0 || d->n_k <= 0 || d->max_q <= 0 || d->max_k <= 0) return CSAT_ERR_SHAPE;
     if (d->Hq % d->Hkv != 0 || d->d % d_multiple != 0 || d->d > 256) return CSAT_ERR_SHAPE;
-    if ((long long)d->B * d->Hq > 0xffffffLL || (long long)d->n_q * d->Hq > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (d->B > kMaxBlocksYZ || (long long)d->B * d->Hq > kMaxBlocks || (long long)d->n_q * d->Hq > kMaxRows) return CSAT_ERR_SHAPE;
     return CSAT_OK;
 }
 // max_q, max_k beyond the packed rows say nothing more
@@ -2209,8 +2211,8 @@ csat_status check_cache(const csat_packed_dims& d, const csat_cache* c) {
     if (!c) return CSAT_ERR_NULL;
     if (c->pages <= 0 || c->max_pages <= 0 || c->max_len <= 0) return CSAT_ERR_SHAPE;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return CSAT_ERR_SHAPE;
-    if ((long long)c->max_pages * c->page < c->max_len || (long long)c->max_pages * c->page > kMaxGrid) return CSAT_ERR_SHAPE;
-    if ((long long)d.B * d.Hkv * ((c->max_len + c->page - 1) / c->page) > kMaxGrid) return CSAT_ERR_SHAPE;
+    if ((long long)c->max_pages * c->page < c->max_len || (long long)c->max_pages * c->page > kMaxRows) return CSAT_ERR_SHAPE;
+    if (2LL * d.Hkv * ((c->max_len + c->page - 1) / c->page) > kMaxBlocks) return CSAT_ERR_SHAPE;
     return CSAT_OK;
 }
 csat_status check_cache_pointers(const csat_cache& c) {
@@ -2827,7 +2829,7 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_offsets) || !aligned16(k_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace))
         return CSAT_ERR_ALIGN;
     const PromptPlan p = prompt_plan(d);
-    if ((long long)d.B * d.Hkv * p.tiles * p.shares > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (p.tiles > kMaxBlocksYZ || (p.shares > 1 && (long long)d.B * longest_q(d) * d.Hq > kMaxBlocks)) return CSAT_ERR_SHAPE;
     if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
     OptionScope scope(ctx);
     hipStream_t st = (hipStream_t)stream;
@@ -2835,14 +2837,14 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.lse = lse; a.q_off = q_offsets; a.k_off = k_offsets;
     a.q_token = d.q_token; a.q_head = d.q_head; a.k_token = d.k_token; a.k_head = d.k_head;
     a.v_token = d.v_token; a.v_head = d.v_head; a.o_token = d.o_token; a.o_head = d.o_head;
-    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.d = d.d; a.n_q = d.n_q; a.n_k = d.n_k; a.max_q = longest_q(d); a.causal = d.causal != 0;
+    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = Group(d.Hq / d.Hkv); a.d = d.d; a.n_q = d.n_q; a.n_k = d.n_k; a.max_q = longest_q(d); a.causal = d.causal != 0;
     a.sl = scale * 1.4426950408889634f;
     a.tiles = p.tiles; a.shares = p.shares; a.part = (float*)workspace;
     Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_PROMPT, st);
     HIP_TRY(d.dtype == CSAT_BF16 ? prompt_launch_bf16(a, p.split, st) : prompt_launch_f32(a, p.split, st));
     if (p.shares > 1) {
         tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
-        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares, nullptr, 0, 0};
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.d, d.n_q, a.max_q, p.shares, nullptr, 0, 0};
         HIP_TRY(d.dtype == CSAT_BF16 ? attention_join_launch_bf16(j, st) : attention_join_launch_f32(j, st));
     }
     return CSAT_OK;
@@ -2865,7 +2867,7 @@ csat_status csat_cache_store(void* ctx, const csat_packed_dims* dims, const csat
     a.c = cache_view(*cache);
     a.K = K; a.V = V; a.k_off = k_offsets;
     a.k_token = d.k_token; a.k_head = d.k_head; a.v_token = d.v_token; a.v_head = d.v_head;
-    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.n_k = d.n_k; a.max_k = longest_k(d);
+    a.B = d.B; a.Hkv = d.Hkv; a.d = d.d; a.n_k = d.n_k; a.max_k = longest_k(d); a.quad_magic = (1 << 20) / (d.d / 4) + 1;
     a.reach = std::min((a.max_k - 1 + cache->page - 1) / cache->page + 1, (cache->max_len + cache->page - 1) / cache->page);
     Timed tm(&static_cast<Context*>(ctx)->prof, CSAT_K_STORE, st);
     HIP_TRY(cache_store_launch(d.dtype == CSAT_BF16, a, st));
@@ -2894,7 +2896,8 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(q_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(W) || !aligned16(workspace)) return CSAT_ERR_ALIGN;
     const CachedPlan p = cached_plan(d, *cache, W != nullptr);
-    if ((long long)d.B * d.Hkv * p.tiles * p.shares > kMaxGrid) return CSAT_ERR_SHAPE;
+    if ((long long)d.Hkv * p.tiles > kMaxBlocks || p.shares > kMaxBlocksYZ ||
+        (long long)d.B * longest_q(d) * d.Hq + (long long)d.B * d.Hkv * ((cache->max_len + 1023) / 1024) > kMaxBlocks) return CSAT_ERR_SHAPE;
     if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
     OptionScope scope(ctx);
     hipStream_t st = (hipStream_t)stream;
@@ -2902,7 +2905,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     a.c = cache_view(*cache);
     a.Q = Q; a.O = O; a.lse = lse; a.q_off = q_offsets;
     a.q_token = d.q_token; a.q_head = d.q_head; a.o_token = d.o_token; a.o_head = d.o_head;
-    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.d = d.d; a.n_q = d.n_q; a.max_q = longest_q(d); a.causal = d.causal != 0;
+    a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = Group(d.Hq / d.Hkv); a.d = d.d; a.n_q = d.n_q; a.max_q = longest_q(d); a.causal = d.causal != 0;
     a.sl = scale * 1.4426950408889634f;
     a.tiles = p.tiles; a.shares = p.shares; a.share_tokens = p.share_tokens;
     a.part = p.part_bytes ? (float*)workspace : nullptr;
@@ -2912,7 +2915,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     HIP_TRY(cache_attention_launch(d.dtype == CSAT_BF16, a, st));
     if (a.part) {
         tl_forms[CSAT_FORM_KEY_SHARES] = p.shares;
-        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.Hkv, a.G, d.d, d.n_q, a.max_q, p.shares, cache->lengths, p.share_tokens, cache->max_len};
+        JoinArgs j{a.part, O, lse, q_offsets, d.o_token, d.o_head, d.B, d.Hq, d.d, d.n_q, a.max_q, p.shares, cache->lengths, p.share_tokens, cache->max_len};
         HIP_TRY(cache_join_launch(d.dtype == CSAT_BF16, j, a, st));
     }
     return CSAT_OK;
@@ -2930,7 +2933,7 @@ csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat
     if (!W || !W_to || !kept) return CSAT_ERR_NULL;
     if (budget < 1 || recent < 0 || recent > budget) return CSAT_ERR_PARAM;
     const int most = std::min(budget, from->max_len);
-    if (from->page != to->page || to->max_len < most || (long long)d.B * d.Hkv * budget > kMaxGrid) return CSAT_ERR_SHAPE;
+    if (from->page != to->page || to->max_len < most || (long long)d.B * d.Hkv * budget > kMaxRows) return CSAT_ERR_SHAPE;
     if (!aligned16(W) || !aligned16(W_to) || !aligned16(kept)) return CSAT_ERR_ALIGN;
     OptionScope scope(ctx);
     hipStream_t st = (hipStream_t)stream;

@@ -54,6 +54,8 @@ struct StoreArgs {
     const int* k_off;
     long long k_token, k_head, v_token, v_head;
     int B, Hkv, d, n_k, max_k, reach;      // reach: pages that one sequence's new tokens may touch
+    int quad_magic;                        // 2^20 / (d / 4) + 1: a piece's row without a division
+    __device__ __forceinline__ int by_row(int q) const { return (int)((uint32_t)q * (uint32_t)quad_magic >> 20); }      // q / (d / 4), q < 2^11
 };
 
 __device__ __forceinline__ float wave_max(float x) {
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     __shared__ float red[2][4];
     extern __shared__ uint4 turned[];                // [d][page + 4] codes of V
     const int tid = threadIdx.x;
-    const int hk = blockIdx.x % a.Hkv, i = blockIdx.x / a.Hkv % a.reach, b = blockIdx.x / a.Hkv / a.reach;
+    const int b = blockIdx.y, i = blockIdx.x / a.Hkv, hk = blockIdx.x - i * a.Hkv;
     const PackedSpan ks(a.k_off, b, a.n_k);
     const int n = ks.count < a.max_k ? ks.count : a.max_k;
     const int len = a.c.lengths[b];
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     Four xk[NI][4], xv[NI][4];
 #pragma unroll
     for (int p = 0; p < NI; ++p) {
-        const int q = p * 256 + tid, s = q / dq * 4, f = q % dq * 4;
+        const int q = p * 256 + tid, i4 = a.by_row(q), s = 4 * i4, f = 4 * (q - i4 * dq);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             xk[p][e] = xv[p][e] = Four{};
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     const int pitch = page + 4;
 #pragma unroll
     for (int p = 0; p < NI; ++p) {
-        const int q = p * 256 + tid, s = q / dq * 4, f = q % dq * 4;
+        const int q = p * 256 + tid, i4 = a.by_row(q), s = 4 * i4, f = 4 * (q - i4 * dq);
         if (q >= items || s + 4 <= lo || s >= hi) continue;
         uint32_t w[4];
 #pragma unroll
@@ -217,12 +219,13 @@ struct CachedArgs {
     float* lse;
     const int* q_off;
     long long q_token, q_head, o_token, o_head;
-    int B, Hq, Hkv, G, d, n_q, max_q, causal;
+    int B, Hq, Hkv, d, n_q, max_q, causal;
+    Group G;
     float sl;                      // scale log2(e)
     int tiles;                     // 16-row tiles per sequence and key head
     int shares, share_tokens;      // the longest sequence's shares of share_tokens (a multiple of 64); a sequence has those it needs
     float* part;                   // [shares][n_q Hq][d], then [shares][n_q Hq][2] as in csat_prompt.h, or null: O and lse are written
-    float* scores;                 // [B][Hkv][max_q G][score_ld] in units of log2, for the weights, or null
+    float* scores;                 // [B][Hkv][max_q G.size][score_ld] in units of log2, for the weights, or null
     int score_ld;
     float* W;                      // [B][Hkv][max_pages page]
     float decay;
@@ -263,17 +266,16 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     extern __shared__ float joint[];                // [4][16][d + 4] outputs, then [4][16][2]; a token per feature, of its first NaN
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int hk = blockIdx.x % a.Hkv, tile = blockIdx.x / a.Hkv % a.tiles, share = blockIdx.x / a.Hkv / a.tiles % a.shares;
-    const int b = blockIdx.x / a.Hkv / a.tiles / a.shares;
+    const int b = blockIdx.z, share = blockIdx.y, tile = a.tiles == 1 ? 0 : blockIdx.x / a.Hkv, hk = blockIdx.x - tile * a.Hkv;
     const PackedSpan qs(a.q_off, b, a.n_q);
-    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G, r_base = 16 * tile;
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size, r_base = 16 * tile;
     if (r_base >= rows) return;
     int L = a.c.lengths[b];
     bool bad = L < 0 || L > a.c.max_len;
     if (bad) L = 0;
     auto limit_of = [&](int r) {
         if (!a.causal) return L;
-        const int v = r / a.G + L - qs.count + 1;
+        const int v = a.G.token(r) + L - qs.count + 1;
         return v < 0 ? 0 : v > L ? L : v;
     };
     const int r_last = r_base + 16 < rows ? r_base + 15 : rows - 1;
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     if (s0 >= L && share > 0) return;
     const int t0 = s0 / 64, t1 = (s1 + 63) / 64;     // (none where no row of the tile sees the share)
     const int r = r_base + li < rows ? r_base + li : rows - 1;
-    const int tok = r / a.G, head = hk * a.G + r % a.G, lim = limit_of(r);
+    const int tok = a.G.token(r), head = hk * a.G.size + r - tok * a.G.size, lim = limit_of(r);
 
     // features 64 c + 16 quad + 8 h .. + 7 of the lane's row
     bf16x8 qf[NP][DC][2];
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
                 if (vt + i >= lim) e[i] = -INFINITY;
         }
         if (a.scores && r_base + li < rows) {
-            float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G + r) * a.score_ld + vt;
+            float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G.size + r) * a.score_ld + vt;
 #pragma unroll
             for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[i], e[i + 1], e[i + 2], e[i + 3]};
         }
@@ -480,11 +482,11 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
             total += k * y.y;
             x[0] += k * z.x; x[1] += k * z.y; x[2] += k * z.z; x[3] += k * z.w;
         }
-        const int rr = r_base + i, h = hk * a.G + rr % a.G, seen = limit_of(rr);
+        const int rr = r_base + i, rt = a.G.token(rr), h = hk * a.G.size + rr - rt * a.G.size, seen = limit_of(rr);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (nan_at[f + e] < seen) x[e] = __uint_as_float(0x7fc00000u);
-        const long long row = qs.first + rr / a.G;
+        const long long row = qs.first + rt;
         if (a.part) {
             const long long all = (long long)a.n_q * a.Hq, at = (long long)share * all + row * a.Hq + h;
             *(float4*)(a.part + at * a.d + f) = float4{x[0], x[1], x[2], x[3]};
@@ -516,14 +518,14 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
     const int L = a.c.lengths[b], t = chunk * 1024 + 4 * tid;
     if (L < 0 || L > a.c.max_len || chunk * 1024 >= L) return;
     const PackedSpan qs(a.q_off, b, a.n_q);
-    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G;
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size;
     const long long all = (long long)a.n_q * a.Hq;
     const float2* ml = (const float2*)(a.part + (long long)a.shares * all * a.d);
     const int shares = shares_of(a.c.lengths, b, a.share_tokens, a.c.max_len, a.shares);
     float* const w = a.W + ((long long)b * a.Hkv + hk) * a.c.max_pages * a.c.page + t;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     // four rows' scores are asked for ahead of what they are weighed with
-    const float* const scores = a.scores + ((long long)b * a.Hkv + hk) * a.max_q * a.G * a.score_ld + t;
+    const float* const scores = a.scores + ((long long)b * a.Hkv + hk) * a.max_q * a.G.size * a.score_ld + t;
     float4 y[4];
     auto ask = [&](int r) {
 #pragma unroll
@@ -534,8 +536,8 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
         const int n = rows - r0 < RB ? rows - r0 : RB;
         __syncthreads();
         for (int i = tid >> 6; i < n; i += 4) {      // a wavefront a row
-            const int r = r0 + i;
-            const long long at = (long long)(qs.first + r / a.G) * a.Hq + hk * a.G + r % a.G;
+            const int r = r0 + i, tok = a.G.token(r);
+            const long long at = (long long)(qs.first + tok) * a.Hq + hk * a.G.size + r - tok * a.G.size;
             const float2 z = lane < shares ? ml[(long long)lane * all + at] : float2{INFINITY, 0.f};      // (the first 64 shares)
             float off = z.x;
             for (int s = lane + 64; s < shares; s += 64) off = fminf(off, ml[(long long)s * all + at].x);
@@ -548,7 +550,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs 
             }
 #pragma unroll
             for (int s = 1; s < 64; s *= 2) total += __shfl_xor(total, s);
-            const int v = a.causal ? r / a.G + L - qs.count + 1 : L;
+            const int v = a.causal ? tok + L - qs.count + 1 : L;
             if (lane == 0) {
                 lse2[i] = total == 0.f ? INFINITY : __log2f(total) - off;      // (nothing seen: weights 0)
                 limit[i] = v < 0 ? 0 : v > L ? L : v;
@@ -680,7 +682,8 @@ static __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(Evi
             if (lane == 63) wsum[wave] = up_to;
             __syncthreads();
             int before = up_to - mine;
-            for (int v = 0; v < wave; ++v) before += wsum[v];
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) before += v < wave ? wsum[v] : 0;
             bins[top] = 0;
             if (per == 2) bins[top - 1] = 0;
             if (before < need && before + mine >= need) {
@@ -748,7 +751,7 @@ __device__ __forceinline__ float largest_code(uint32_t w) {      // (the maximum
     return fmaxf(fmaxf(fabsf(lo[0]), fabsf(lo[1])), fmaxf(fabsf(hi[0]), fabsf(hi[1])));
 }
 template <int NI>      // 16-byte pieces per thread; (six workgroups per CU: 109 us where five take 120, 112 k tokens cut to half)
-__global__ __launch_bounds__(256, NI <= 2 ? 6 : NI == 4 ? 3 : 1) void cache_gather_kernel(EvictArgs a, int blocks) {
+__global__ __launch_bounds__(256, NI <= 2 ? 6 : NI == 4 ? 3 : 1) void cache_gather_kernel(EvictArgs a) {
     extern __shared__ uint4 staged[];
     __shared__ long long src_block[128];      // page * Hkv + head
     __shared__ int src_slot[128];             // K: slot in the source page; V: its byte among the staged rows of its round
@@ -757,7 +760,7 @@ __global__ __launch_bounds__(256, NI <= 2 ? 6 : NI == 4 ? 3 : 1) void cache_gath
     __shared__ float red[4];
     __shared__ int different, in_first;
     const int tid = threadIdx.x, lane = tid & 63, page = a.from.page, d = a.d;
-    const int hk = blockIdx.x % a.Hkv, is_v = blockIdx.x / a.Hkv % 2, j = blockIdx.x / a.Hkv / 2 % blocks, b = blockIdx.x / a.Hkv / 2 / blocks;
+    const int b = blockIdx.y, both = blockIdx.x / a.Hkv, hk = blockIdx.x - both * a.Hkv, is_v = both & 1, j = both >> 1;
     const int* const kept = a.kept + ((long long)b * a.Hkv + hk) * a.budget + (long long)j * page;
     const int* const table = a.from.table + (long long)b * a.from.max_pages;
     // (the slots are asked for before it is known how many there are: -1 behind them)

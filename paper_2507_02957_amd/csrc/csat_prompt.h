@@ -16,13 +16,24 @@
 
 namespace csat {
 
+// Query heads to a key head; the rows of a key head are its (token, head of the group) pairs.
+struct Group {
+    int size, shift;               // shift >= 0: size is that power of two
+    __host__ __device__ Group(int n = 1) : size(n), shift(-1) {
+        for (int k = 0; k < 31; ++k)
+            if (n == 1 << k) shift = k;
+    }
+    __device__ __forceinline__ int token(int r) const { return shift >= 0 ? r >> shift : r / size; }
+};
+
 struct PromptArgs {
     const void *Q, *K, *V;
     void* O;
     float* lse;
     const int *q_off, *k_off;
     long long q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
-    int B, Hq, Hkv, G, d, n_q, n_k, max_q, causal;
+    int B, Hq, Hkv, d, n_q, n_k, max_q, causal;
+    Group G;
     float sl;                      // scale log2(e)
     int tiles;                     // row tiles per sequence and key head
     int shares;                    // > 1: workgroups that split a row tile's keys, joined by attention_join_kernel
@@ -172,7 +183,8 @@ struct PromptRows : PromptAcc<DT> {
         const int lh = lane >> 5, dc = a.d / EPC;
         this->clear();
         this->lim = limit;
-        const T* q = (const T*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
+        const int token = a.G.token(r);
+        const T* q = (const T*)a.Q + (long long)(first + token) * a.q_token + (long long)(hk * a.G.size + r - token * a.G.size) * a.q_head;
         if (dc == C) {
 #pragma unroll
             for (int g = 0; g < NK; ++g) qf[g] = *(const uint4*)(q + (2 * g + lh) * EPC);
@@ -265,7 +277,8 @@ struct PromptRowsParts : PromptAcc<DT> {
         const int lh = lane >> 5;
         this->clear();
         this->lim = limit;
-        const float* q = (const float*)a.Q + (long long)(first + r / a.G) * a.q_token + (long long)(hk * a.G + r % a.G) * a.q_head;
+        const int token = a.G.token(r);
+        const float* q = (const float*)a.Q + (long long)(first + token) * a.q_token + (long long)(hk * a.G.size + r - token * a.G.size) * a.q_head;
 #pragma unroll
         for (int g = 0; g < NB; ++g) {
             const int f = 16 * g + 8 * lh;
@@ -398,18 +411,15 @@ __device__ __forceinline__ void wait_staged() { __builtin_amdgcn_s_waitcnt(0x0f7
 // take different heads, so an XCD's keep to a share of the heads where their number is a multiple of eight.
 template <int ROWS>
 struct PromptPlace {
-    int share, b, hk, r_base, rows, r_end, lo, hi, q_first, q_count, k_first, nk, G, causal;
-    __device__ __forceinline__ explicit PromptPlace(const PromptArgs& a) {
-        const int P = a.B * a.Hkv, id = blockIdx.x % (P * a.tiles), pair = id % P;
-        share = blockIdx.x / (P * a.tiles);
-        b = pair / a.Hkv;
-        hk = pair % a.Hkv;
-        G = a.G;
-        causal = a.causal;
+    int share, b, hk, r_base, rows, r_end, lo, hi, q_first, q_count, k_first, nk, causal;
+    Group G;
+    __device__ __forceinline__ explicit PromptPlace(const PromptArgs& a) : share(blockIdx.z), causal(a.causal), G(a.G) {
+        b = blockIdx.x / a.Hkv;
+        hk = blockIdx.x - b * a.Hkv;
         const PackedSpan qs(a.q_off, b, a.n_q), ks(a.k_off, b, a.n_k);
         q_first = qs.first; q_count = qs.count; k_first = ks.first; nk = ks.count;
-        rows = (q_count < a.max_q ? q_count : a.max_q) * G;
-        r_base = (a.tiles - 1 - id / P) * ROWS;
+        rows = (q_count < a.max_q ? q_count : a.max_q) * G.size;
+        r_base = (a.tiles - 1 - (int)blockIdx.y) * ROWS;
         r_end = r_base + ROWS < rows ? r_base + ROWS : rows;
         lo = r_base < rows ? limit(r_base) : 0;
         hi = r_base < rows ? limit(r_end - 1) : 0;
@@ -427,7 +437,7 @@ struct PromptPlace {
     }
     __device__ __forceinline__ int limit(int r) const {      // keys that row r sees
         if (!causal) return nk;
-        const int v = r / G + nk - q_count + 1;
+        const int v = G.token(r) + nk - q_count + 1;
         return v < 0 ? 0 : v > nk ? nk : v;
     }
 };
@@ -480,8 +490,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     if (!active) return;
 
     const float total = pair_sum(rows.sum);
-    const int head = at.hk * a.G + r % a.G;
-    const long long row = at.q_first + r / a.G;
+    const int token = a.G.token(r), head = at.hk * a.G.size + r - token * a.G.size;
+    const long long row = at.q_first + token;
     f32x16 (&o)[DT] = rows.o;
     if (*any_odd) {
 #pragma unroll
@@ -608,8 +618,8 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
     const int n = at.r_end - at.r_base, dq = a.d / 4;
     const bool odd = *any_odd != 0;
     for (int q = tid; q < n * dq; q += THREADS) {
-        const int i = q / dq, c = q % dq * 4, r = at.r_base + i, head = at.hk * a.G + r % a.G;
-        const long long row = at.q_first + r / a.G;
+        const int i = q / dq, c = q % dq * 4, r = at.r_base + i, token = a.G.token(r), head = at.hk * a.G.size + r - token * a.G.size;
+        const long long row = at.q_first + token;
         float off = INFINITY, total = 0.f;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -647,7 +657,7 @@ struct JoinArgs {
     float* lse;
     const int* q_off;
     long long o_token, o_head;
-    int B, Hq, Hkv, G, d, n_q, max_q, shares;
+    int B, Hq, d, n_q, max_q, shares;
     const int* lengths;            // the sequences' keys, where a share is `share_keys` of them and a sequence has only those it needs; or null
     int share_keys, max_len;
 };

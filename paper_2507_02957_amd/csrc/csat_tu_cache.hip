@@ -5,25 +5,25 @@
 namespace csat {
 
 template <typename K, typename... A>
-static hipError_t launch(K kernel, long long grid, int threads, int lds_bytes, hipStream_t st, A... args) {
+static hipError_t launch(K kernel, dim3 grid, int threads, int lds_bytes, hipStream_t st, A... args) {
     if (lds_bytes > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), lds_bytes, st, args...);
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds_bytes, st, args...);
     return hipGetLastError();
 }
 
 hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st) {
-    const int items = (a.d * a.c.page / 16 + 255) / 256;
-#define CSAT_STORE(NI_) (bf16 ? launch(cache_store_kernel<bf16_t, NI_>, (long long)a.B * a.reach * a.Hkv, 256, store_lds_bytes(a.d, a.c.page), st, a) \
-                              : launch(cache_store_kernel<float, NI_>, (long long)a.B * a.reach * a.Hkv, 256, store_lds_bytes(a.d, a.c.page), st, a))
+    const int items = (a.d * a.c.page / 16 + 255) / 256, lds_bytes = store_lds_bytes(a.d, a.c.page);
+    const dim3 grid((unsigned)(a.Hkv * a.reach), (unsigned)a.B);
+#define CSAT_STORE(NI_) (bf16 ? launch(cache_store_kernel<bf16_t, NI_>, grid, 256, lds_bytes, st, a) : launch(cache_store_kernel<float, NI_>, grid, 256, lds_bytes, st, a))
     return items <= 1 ? CSAT_STORE(1) : items <= 2 ? CSAT_STORE(2) : items <= 4 ? CSAT_STORE(4) : CSAT_STORE(8);
 #undef CSAT_STORE
 }
 
 hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st) {
-    const long long grid = (long long)a.B * a.shares * a.tiles * a.Hkv;
+    const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.shares, (unsigned)a.B);
 #define CSAT_CACHED(DC_) (bf16 ? launch(cache_attention_kernel<bf16_t, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a) \
                                : launch(cache_attention_kernel<float, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a))
     if (a.d <= 64) return CSAT_CACHED(1);
@@ -41,11 +41,11 @@ hipError_t cache_join_launch(bool bf16, const JoinArgs& j, const CachedArgs& a, 
 }
 
 hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st) {
-    const hipError_t e = launch(cache_select_kernel, (long long)a.B * a.Hkv, kSelectThreads, 0, st, a);
+    const hipError_t e = launch(cache_select_kernel, dim3((unsigned)(a.B * a.Hkv)), kSelectThreads, 0, st, a);
     if (e != hipSuccess) return e;
     const int items = (a.d * a.from.page / 16 + 255) / 256, lds_bytes = gather_pages(a.d, a.from.page) * gather_page_bytes(a.d, a.from.page);
-    const long long grid = (long long)a.B * blocks * 2 * a.Hkv;
-#define CSAT_GATHER(NI_) launch(cache_gather_kernel<NI_>, grid, 256, lds_bytes, st, a, blocks)
+    const dim3 grid((unsigned)(a.Hkv * 2 * blocks), (unsigned)a.B);
+#define CSAT_GATHER(NI_) launch(cache_gather_kernel<NI_>, grid, 256, lds_bytes, st, a)
     return items <= 1 ? CSAT_GATHER(1) : items <= 2 ? CSAT_GATHER(2) : items <= 4 ? CSAT_GATHER(4) : CSAT_GATHER(8);
 #undef CSAT_GATHER
 }

@@ -247,10 +247,11 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
  * q_offsets[b+1], those of K and V k_offsets[b] .. k_offsets[b+1] (device int32 [B+1], not decreasing, within
  * n_q / n_k; sequences may be empty).  Row r, head h starts at element r * token stride + h * head stride of its
  * tensor; strides are multiples of 16 bytes (so a part of a fused projection serves as well as a tensor of its own, and 0
- * repeats a row), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
+ * repeats a row, except of O, whose rows must not lie on one another), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
  * max_q, max_k bound the rows of one sequence: rows beyond the bound are not computed and not written.  So are rows
  * of no sequence (behind the last offset): they are left as they were.
- * d: a multiple of 8 (csat_prompt_attention) or of 16 (the cache), at most 256.  n_q, n_k, max_q, max_k at least 1.
+ * d: a multiple of 8 (csat_prompt_attention) or of 16 (the cache), at most 256.  n_q, n_k, max_q, max_k at least 1; B at most
+ * 65535, n_q * Hq, n_k and a cache's max_pages * page at most 2^30.
  * ------------------------------------------------------------------------------------------------------ */
 typedef struct {
     int B, Hq, Hkv, d;
@@ -277,9 +278,10 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
  * attention's matrix instructions take them).  A sequence's tokens are the first lengths[b] slots of the pages that row b of
  * table (device int32 [B, max_pages]) names; entries beyond them are not read.  max_len bounds lengths[b] (it sizes
  * the grids; at most max_pages * page).  Pages may be shared by sequences as long as they are only read.
- * Errors in what only the device sees: a sequence whose length is negative or above max_len, or one of whose needed
- * table entries names no page of the pool, gives NaN in its rows of O and lse (its weights are then undefined), is not
- * stored to, and is evicted to length -1 with nothing else written for it; memory outside the given tensors is never touched. */
+ * Errors in what only the device sees: a sequence whose length is negative or above max_len (to store: or below the new
+ * rows), or one of whose needed table entries names no page of the pool, gives NaN in its rows of O and lse (its weights are then
+ * undefined), is not stored to, and is evicted to length -1 with nothing but kept = -1 written for it; memory outside the given
+ * tensors is never touched. */
 typedef struct {
     int pages, page, max_pages, max_len;
     void *K, *V;
@@ -312,7 +314,8 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
  * order to the pages of `to` (which must be none of the pages read; their pools may be the same, page sizes must be), blocks with
  * the smallest scale for what they hold; W_to [B, Hkv, to->max_pages * page] gets their weights,
  * kept [B, Hkv, budget] int32 their slots in `from` (-1 behind them), to->lengths their number.  Every head keeps tokens of its own.
- * to->max_len and to->max_pages * page must be at least min(budget, from->max_len), else CSAT_ERR_SHAPE. */
+ * to->max_len and to->max_pages * page must be at least min(budget, from->max_len), else CSAT_ERR_SHAPE; W_to, to->table and
+ * to->lengths must be others than W, from->table and from->lengths (other heads still read those), else CSAT_ERR_PARAM. */
 csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat_cache* from, const csat_cache* to,
                              const float* W, float* W_to, int budget, int recent, int* kept, void* stream);
 

@@ -373,11 +373,14 @@ def _issue(entry, t, stream, args):
     without a stream object."""
     import torch
     index = t.device.index
-    if index != torch.cuda.current_device():
+    if index is None:
+        raise ValueError("the tensors must be on a GPU")
+    fn = getattr(_lib or load_library(), entry)
+    if index == torch.cuda.current_device():
+        status = fn(_ctx or context(), *args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    else:
         with torch.cuda.device(index):
-            return _issue(entry, t, stream, args)
-    st = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-    status = getattr(_lib or load_library(), entry)(_ctx or context(), *args, st)
+            status = fn(_ctx or context(), *args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
     if status != 0:
         _check(status)
 

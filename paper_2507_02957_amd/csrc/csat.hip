@@ -2170,11 +2170,13 @@ bool hadamard_fits_lds(int n, int m) {
 
 // ---- Exact attention over packed sequences and the 8-bit cache (csat_prompt.h, csat_cache.h)
 
-constexpr long long kMaxRows = 0x7fffffffLL;
+constexpr long long kMaxRows = 1 << 30;              // rows, tokens, slots: the kernels count them, and a step beyond them, in 32 bits
 constexpr long long kMaxBlocks = (1 << 22) - 1;      // workgroups of up to 1024 threads along x ...
 constexpr long long kMaxBlocksYZ = 65535;            // ... and along y and z
 constexpr long long kMaxTokenStride = 1 << 24;
 
+// rows of O must not lie on one another
+bool output_strides_ok(const csat_packed_dims& d) { return (d.n_q == 1 || d.o_token >= d.d) && (d.Hq == 1 || d.o_head >= d.d); }
 bool stride_ok(long long token, long long head, size_t e) {
     return token >= 0 && token < kMaxTokenStride && head >= 0 && token * (long long)e % 16 == 0 && head * (long long)e % 16 == 0;
 }
@@ -2183,7 +2185,7 @@ csat_status check_packed(const csat_packed_dims* d, int d_multiple) {
     if (d->dtype != CSAT_F32 && d->dtype != CSAT_BF16) return CSAT_ERR_DTYPE;
     if (d->B <= 0 || d->Hq <= 0 || d->Hkv <= 0 || d->d <= 0 || d->n_q <= 0 || d->n_k <= 0 || d->max_q <= 0 || d->max_k <= 0) return CSAT_ERR_SHAPE;
     if (d->Hq % d->Hkv != 0 || d->d % d_multiple != 0 || d->d > 256) return CSAT_ERR_SHAPE;
-    if (d->B > kMaxBlocksYZ || (long long)d->B * d->Hq > kMaxBlocks || (long long)d->n_q * d->Hq > kMaxRows) return CSAT_ERR_SHAPE;
+    if (d->B > kMaxBlocksYZ || (long long)d->B * d->Hq > kMaxBlocks || (long long)d->n_q * d->Hq > kMaxRows || d->n_k > kMaxRows) return CSAT_ERR_SHAPE;
     return CSAT_OK;
 }
 // max_q, max_k beyond the packed rows say nothing more
@@ -2823,7 +2825,7 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     const csat_packed_dims& d = *dims;
     const size_t e = esize(d.dtype);
     if (!Q || !K || !V || !q_offsets || !k_offsets || !O) return CSAT_ERR_NULL;
-    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.k_token, d.k_head, e) || !stride_ok(d.v_token, d.v_head, e) || !stride_ok(d.o_token, d.o_head, e))
+    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.k_token, d.k_head, e) || !stride_ok(d.v_token, d.v_head, e) || !stride_ok(d.o_token, d.o_head, e) || !output_strides_ok(d))
         return CSAT_ERR_SHAPE;
     if (!(scale > 0.f) || !std::isfinite(scale)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_offsets) || !aligned16(k_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace))
@@ -2892,7 +2894,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     CSAT_TRY(check_cache_pointers(*cache));
     if (!Q || !q_offsets || !O) return CSAT_ERR_NULL;
     const size_t e = esize(d.dtype);
-    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.o_token, d.o_head, e)) return CSAT_ERR_SHAPE;
+    if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.o_token, d.o_head, e) || !output_strides_ok(d)) return CSAT_ERR_SHAPE;
     if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(q_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(W) || !aligned16(workspace)) return CSAT_ERR_ALIGN;
     const CachedPlan p = cached_plan(d, *cache, W != nullptr);
@@ -2932,6 +2934,7 @@ csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat
     CSAT_TRY(check_cache_pointers(*to));
     if (!W || !W_to || !kept) return CSAT_ERR_NULL;
     if (budget < 1 || recent < 0 || recent > budget) return CSAT_ERR_PARAM;
+    if (W == W_to || from->lengths == to->lengths || from->table == to->table) return CSAT_ERR_PARAM;
     const int most = std::min(budget, from->max_len);
     if (from->page != to->page || to->max_len < most || (long long)d.B * d.Hkv * budget > kMaxRows) return CSAT_ERR_SHAPE;
     if (!aligned16(W) || !aligned16(W_to) || !aligned16(kept)) return CSAT_ERR_ALIGN;

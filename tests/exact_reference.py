@@ -5,6 +5,7 @@ import numpy as np
 import torch
 
 E4M3_MAX, SCALE_MIN = 448.0, -118
+TINY = 2.0 ** -126        # matrix instructions may take what is smaller as 0
 
 
 def half_step(dtype):
@@ -39,10 +40,10 @@ def attend(q, k, v, limit, scale, dtype):
                 continue
             ds = eps * (q.shape[1] + 8) * scale * (np.abs(k[:c][vis]) @ np.abs(q[i])).max()
             w = 2 * ds + eps * (keys + 32)
-            dP[i, :c] = w * p + 1e-37
+            dP[i, :c] = w * p + TINY
             dlse[i] = ds + eps * (keys + 32) + 2 * eps * abs(lse[i])
             wv = w + (half_step(dtype) if dtype == "bf16" else 0.0)
-            dO[i] = wv * (p[vis][:, None] * np.abs(v[:c][vis])).sum(0) + half_step(dtype) * np.abs(O[i]) * (1 + wv) + 1e-37
+            dO[i] = wv * (p[vis][:, None] * np.abs(v[:c][vis])).sum(0) + half_step(dtype) * np.abs(O[i]) * (1 + wv) + 2 * TINY
     return O, lse, P, dO, dlse, dP
 
 

@@ -36,7 +36,7 @@ def _cache(**kw):
 
 
 BAD_DIMS = [(dict(B=0), -2), (dict(Hq=3), -2), (dict(Hkv=0), -2), (dict(d=12), -2), (dict(d=264), -2), (dict(n_q=0), -2), (dict(n_k=-1), -2),
-            (dict(max_q=0), -2), (dict(max_k=0), -2), (dict(dtype=7), -3), (dict(B=1 << 24), -2), (dict(n_q=1 << 30), -2)]
+            (dict(max_q=0), -2), (dict(max_k=0), -2), (dict(dtype=7), -3), (dict(B=65536), -2), (dict(n_q=1 << 29), -2), (dict(n_k=(1 << 30) + 1), -2)]
 BAD_CACHE = [(dict(pages=0), -2), (dict(page=48), -2), (dict(page=256), -2), (dict(page=8), -2), (dict(max_pages=0), -2), (dict(max_len=0), -2),
              (dict(max_len=49), -2), (dict(max_pages=1 << 28), -2)]
 BAD_CACHE_POINTERS = [(dict([(k, None)]), -1) for k in ("K", "V", "Ks", "Vs", "table", "lengths")] + [(dict(K=0x1008), -4), (dict(table=0x1004), -4)]
@@ -54,7 +54,14 @@ def _attend(lib, d, c, Q=P, qo=P, scale=1.0, decay=0.0, O=P, lse=None, W=None, w
     return lib.csat_cache_attention(csat.context(), ctypes.byref(d), ctypes.byref(c), Q, qo, scale, decay, O, lse, W, ws, n, None)
 
 
-def _evict(lib, d, c, to, W=P, W_to=P, budget=20, recent=4, kept=P):
+P2 = ctypes.c_void_p(0x2000)
+
+
+def _to(**kw):
+    return _cache(**{**dict(table=0x2000, lengths=0x2000), **kw})
+
+
+def _evict(lib, d, c, to, W=P, W_to=P2, budget=20, recent=4, kept=P):
     return lib.csat_cache_evict(csat.context(), ctypes.byref(d), ctypes.byref(c), ctypes.byref(to), W, W_to, budget, recent, kept, None)
 
 
@@ -64,7 +71,7 @@ def test_dims_are_refused(lib, change, code):
     n = ctypes.c_size_t()
     assert lib.csat_prompt_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == code
     assert lib.csat_cache_workspace_bytes(ctypes.byref(d), ctypes.byref(c), ctypes.byref(n)) == code
-    assert _prompt(lib, d) == code and _store(lib, d, c) == code and _attend(lib, d, c) == code and _evict(lib, d, c, c) == code
+    assert _prompt(lib, d) == code and _store(lib, d, c) == code and _attend(lib, d, c) == code and _evict(lib, d, c, _to()) == code
 
 
 @pytest.mark.parametrize("change,code", BAD_CACHE + BAD_CACHE_POINTERS)
@@ -73,7 +80,7 @@ def test_caches_are_refused(lib, change, code):
     n = ctypes.c_size_t()
     if (change, code) in BAD_CACHE:
         assert lib.csat_cache_workspace_bytes(ctypes.byref(d), ctypes.byref(c), ctypes.byref(n)) == code
-    assert _store(lib, d, c) == code and _attend(lib, d, c) == code and _evict(lib, d, c, _cache()) == code and _evict(lib, d, _cache(), c) == code
+    assert _store(lib, d, c) == code and _attend(lib, d, c) == code and _evict(lib, d, c, _to()) == code and _evict(lib, d, _cache(), _to(**change)) == code
 
 
 def test_arguments_are_refused(lib):
@@ -90,13 +97,15 @@ def test_arguments_are_refused(lib):
         assert _attend(lib, d, c, **{name: None}) == -1 and _attend(lib, d, c, **{name: ODD}) == -4, name
     assert _attend(lib, d, c, W=ODD) == -4 and _attend(lib, d, c, lse=ODD) == -4
     for name in ("W", "W_to", "kept"):
-        assert _evict(lib, d, c, c, **{name: None}) == -1 and _evict(lib, d, c, c, **{name: ODD}) == -4, name
+        assert _evict(lib, d, c, _to(), **{name: None}) == -1 and _evict(lib, d, c, _to(), **{name: ODD}) == -4, name
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert _prompt(lib, d, scale=scale) == -6 and _attend(lib, d, c, scale=scale) == -6
     for decay in (-0.1, 1.1, float("nan")):
         assert _attend(lib, d, c, decay=decay) == -6
-    assert _evict(lib, d, c, c, budget=0) == -6 and _evict(lib, d, c, c, recent=-1) == -6 and _evict(lib, d, c, c, recent=21) == -6
-    assert _evict(lib, d, c, _cache(max_len=19)) == -2 and _evict(lib, d, c, _cache(page=32)) == -2
+    assert _evict(lib, d, c, _to(), budget=0) == -6 and _evict(lib, d, c, _to(), recent=-1) == -6 and _evict(lib, d, c, _to(), recent=21) == -6
+    assert _evict(lib, d, c, _to(max_len=19)) == -2 and _evict(lib, d, c, _to(page=32)) == -2
+    # what other heads still read is not written over
+    assert _evict(lib, d, c, _to(), W_to=P) == -6 and _evict(lib, d, c, _to(table=0x1000)) == -6 and _evict(lib, d, c, _to(lengths=0x1000)) == -6
 
 
 @pytest.mark.parametrize("name,value", [(t + kind, v) for t in "qkvo" for kind, values in (("_token", (-8, 12, 1 << 24)), ("_head", (-8, 12))) for v in values])
@@ -107,6 +116,17 @@ def test_strides_are_refused(lib, name, value):
         assert _store(lib, d, c) == -2
     else:
         assert _attend(lib, d, c) == -2
+
+
+def test_rows_of_the_output_that_overlap_are_refused(lib):
+    for change in (dict(o_token=0), dict(o_head=0), dict(o_token=24), dict(o_head=24)):
+        assert _prompt(lib, _dims(**change)) == -2 and _attend(lib, _dims(**change), _cache()) == -2
+
+
+def test_tensors_of_the_host_are_refused(lib):
+    x = torch.zeros(10, 4, 32, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        csat.csat_prompt_attention(_dims(), x, x, x, x, x, 1.0, x, None, None)
 
 
 def test_workspaces_are_refused(lib):

@@ -79,6 +79,32 @@ def test_against_the_definition(shape, causal, dtype):
     Problem(q_lens, k_lens, Hq, Hkv, d, dtype, causal, seed=shape).call().check()
 
 
+# enough heads that bf16 takes row tiles of 128 rows
+WIDE = [
+    ([1, 70, 33, 129, 64, 5, 0, 90], [1, 70, 33, 129, 64, 5, 0, 90], 32, 32, 64),
+    ([40, 20, 128, 3], [90, 20, 300, 130], 64, 32, 128),
+    ([130, 7, 60, 64], [65, 9, 64, 200], 32, 32, 80),
+    ([33, 65], [33, 129], 128, 64, 96),
+    ([50, 129], [50, 129], 64, 64, 256),
+    ([140, 31], [100, 31], 64, 64, 200),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", range(len(WIDE)))
+def test_many_heads_against_the_definition(shape, causal):
+    q_lens, k_lens, Hq, Hkv, d = WIDE[shape]
+    Problem(q_lens, k_lens, Hq, Hkv, d, "bf16", causal, seed=shape).call().check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_shares_and_many_rows(dtype):
+    """Two shares of the keys, joined a wavefront a row."""
+    p = Problem([90, 50], [700, 520], 4, 2, 40, dtype, True).call()
+    assert csat.csat_profile_launch_form("key_shares") == 2
+    p.check()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("q_lens,k_lens,Hq,Hkv,d", [([1], [3000], 4, 2, 64), ([1, 3, 0], [2100, 257, 900], 4, 1, 128), ([20], [5000], 2, 2, 80), ([2], [1030], 8, 1, 256)])
 def test_few_rows_share_their_keys(q_lens, k_lens, Hq, Hkv, d, dtype):
@@ -117,11 +143,10 @@ def test_strides(dtype):
 ODD = [float("nan"), float("inf"), -float("inf")]
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("d", [64, 128])
-def test_odd_values_in_masked_places(d, dtype):
+@pytest.mark.parametrize("heads,d,dtype", [(2, 64, "f32"), (2, 128, "f32"), (2, 256, "f32"), (2, 64, "bf16"), (2, 128, "bf16"), (64, 64, "bf16"), (64, 128, "bf16")])
+def test_odd_values_in_masked_places(heads, d, dtype):
     """What no row sees does not matter: rows of no sequence, of the next one, of keys behind the causal limit."""
-    p = Problem([70, 90], [70, 90], 4, 2, d, dtype, True).call().check()
+    p = Problem([70, 90], [70, 90], heads if heads > 2 else 4, heads, d, dtype, True).call().check()
     want, lse = p.O.clone(), p.lse.clone()
     a, b = p.k_off[1], p.k_off[2]
     for i, x in enumerate(ODD):
@@ -136,6 +161,16 @@ def test_odd_values_in_masked_places(d, dtype):
     p.V[a - 2, 0, 11], p.V[a - 1, 0, 11] = ODD[1], ODD[2]            # +inf and -inf together
     p.call().check()
     p.K[a - 30] = float("nan")
+    p.call().check()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-38, 1e30])
+def test_float_values_of_every_size(scale):
+    """V far from 1, where parts of a float are below or next to the smallest bf16 or the largest."""
+    p = Problem([60], [60], 2, 1, 64, "f32", True)
+    p.V *= scale
+    p.call().check()
+    p.V[::3] *= 1e-6
     p.call().check()
 
 

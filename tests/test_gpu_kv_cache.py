@@ -201,6 +201,16 @@ def test_attention_in_shares(dtype):
     s.check_attention(r, *few)
 
 
+def test_attention_in_many_shares():
+    """More shares than a wavefront has lanes, with weights, next to a sequence of one token."""
+    s = Serving(2, 2, 1, 16, 128, 330, "bf16")
+    s.lengths[0] += dev_ints([42000, 1])
+    W = s.weights(2.0)
+    got = s.attend([2, 1], W=W, decay=0.5)
+    assert csat.csat_profile_launch_form("key_shares") > 64
+    s.check_attention(s.reference(), *got, W=W, W_before=np.full(W.shape, 2.0), decay=0.5)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_nan_codes(dtype):
     """NaN codes behind the last token and in tokens that a row does not see have no effect; a row that sees one is NaN there."""
@@ -314,6 +324,15 @@ def test_eviction(page, d, Hkv, lens, budget, recent):
     s.Ks *= torch.exp2(torch.randint(-12, 12, s.Ks.shape, device=DEV).float())
     W = torch.exp(3 * torch.randn(s.weights().shape, device=DEV))
     evict_and_check(s, W, budget, recent)
+
+
+@pytest.mark.parametrize("levels", [0, 7])
+def test_eviction_of_long_sequences(levels):
+    """Longer than the selection holds in registers; weights of their own and ones with many ties."""
+    s = Serving(2, 1, 1, 16, 128, 160, "bf16", tables=2)
+    s.lengths[0] += dev_ints([20000, 8193])
+    W = torch.exp(3 * torch.randn(s.weights().shape, device=DEV)) if levels == 0 else torch.randint(0, levels, s.weights().shape, device=DEV).float()
+    evict_and_check(s, W, 8191, 100)
 
 
 @pytest.mark.parametrize("kind", ["zeros", "equal", "few", "odd", "close"])

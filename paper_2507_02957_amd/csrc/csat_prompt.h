@@ -36,6 +36,7 @@ struct PromptArgs {
     Group G;
     float sl;                      // scale log2(e)
     int tiles;                     // row tiles per sequence and key head
+    int pair_groups;               // (sequence, key head) pairs / the grid's x
     int shares;                    // > 1: workgroups that split a row tile's keys, joined by attention_join_kernel
     float* part;                   // [shares][n_q Hq][d] unnormalised outputs, then [shares][n_q Hq][2]: offset, sum
 };
@@ -407,15 +408,19 @@ struct PromptKeys {
 };
 __device__ __forceinline__ void wait_staged() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0): this wavefront's pieces are there
 
-// Which rows a workgroup has.  Of `tiles` row tiles of ROWS the last, which see most keys, come first; neighbouring workgroups
-// take different heads, so an XCD's keep to a share of the heads where their number is a multiple of eight.
+// Which rows a workgroup has.  The grid's y is a row tile, the last ones, which see most keys, first.  x is a (sequence, key head)
+// pair, z a share of its keys; or, for many tiles, x one of eight pairs and z which eight, so that an XCD, which takes every
+// eighth workgroup, works through the tiles of one pair before the next and finds its keys in its L2.
 template <int ROWS>
 struct PromptPlace {
     int share, b, hk, r_base, rows, r_end, lo, hi, q_first, q_count, k_first, nk, causal;
     Group G;
-    __device__ __forceinline__ explicit PromptPlace(const PromptArgs& a) : share(blockIdx.z), causal(a.causal), G(a.G) {
-        b = blockIdx.x / a.Hkv;
-        hk = blockIdx.x - b * a.Hkv;
+    __device__ __forceinline__ explicit PromptPlace(const PromptArgs& a) : share(0), causal(a.causal), G(a.G) {
+        int pair = blockIdx.x;
+        if (a.shares > 1) share = blockIdx.z;
+        else pair += gridDim.x * blockIdx.z;
+        b = pair / a.Hkv;
+        hk = pair - b * a.Hkv;
         const PackedSpan qs(a.q_off, b, a.n_q), ks(a.k_off, b, a.n_k);
         q_first = qs.first; q_count = qs.count; k_first = ks.first; nk = ks.count;
         rows = (q_count < a.max_q ? q_count : a.max_q) * G.size;

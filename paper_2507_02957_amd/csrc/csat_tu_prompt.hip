@@ -22,7 +22,7 @@ hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, bool split, hipStream_
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.Hkv), (unsigned)a.tiles, (unsigned)a.shares), dim3(threads), lds_bytes, st, a);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.Hkv / a.pair_groups), (unsigned)a.tiles, (unsigned)(a.shares > 1 ? a.shares : a.pair_groups)), dim3(threads), lds_bytes, st, a);
         return hipGetLastError();
     };
 #if CSAT_TU_BF16

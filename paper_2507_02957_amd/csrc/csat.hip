@@ -2230,14 +2230,15 @@ CacheView cache_view(const csat_cache& c) {
     return v;
 }
 
-struct CachedPlan { int tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; };
+struct CachedPlan { int row_tiles, tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; };
 // Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike: 512, more where a
 // sequence would have more shares than it takes to occupy the chip twice (one sequence of 131072 tokens, 8 key heads: 58 us with
 // shares of 2048, 63, 72, 92 with 1024, 512, 256, whose join grows; 32 sequences of 700 to 8100: 92 us with 512, 100 with 2048).
 CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weights) {
     CachedPlan p{};
     const long long rows = (long long)longest_q(d) * (d.Hq / d.Hkv);
-    p.tiles = (int)((rows + 15) / 16);
+    p.row_tiles = rows > 16 && d.dtype == CSAT_BF16 && d.d <= 128 ? 2 : 1;
+    p.tiles = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     const long long groups = (long long)d.B * d.Hkv * p.tiles, most = std::max({512 / groups, std::min(64LL, 8192 / groups), 16LL});
     p.share_tokens = (int)std::max(512LL, round_up((c.max_len + most - 1) / most, 256));
     p.shares = (c.max_len + p.share_tokens - 1) / p.share_tokens;
@@ -2913,7 +2914,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     a.q_token = d.q_token; a.q_head = d.q_head; a.o_token = d.o_token; a.o_head = d.o_head;
     a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = Group(d.Hq / d.Hkv); a.d = d.d; a.n_q = d.n_q; a.max_q = longest_q(d); a.causal = d.causal != 0;
     a.sl = scale * 1.4426950408889634f;
-    a.tiles = p.tiles; a.shares = p.shares; a.share_tokens = p.share_tokens;
+    a.tiles = p.tiles; a.row_tiles = p.row_tiles; a.shares = p.shares; a.share_tokens = p.share_tokens;
     a.part = p.part_bytes ? (float*)workspace : nullptr;
     a.scores = W ? (float*)((char*)workspace + p.part_bytes) : nullptr;
     a.score_ld = p.score_ld; a.W = W; a.decay = decay;

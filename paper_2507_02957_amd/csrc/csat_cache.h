@@ -222,7 +222,7 @@ struct CachedArgs {
     int B, Hq, Hkv, d, n_q, max_q, causal;
     Group G;
     float sl;                      // scale log2(e)
-    int tiles;                     // 16-row tiles per sequence and key head
+    int tiles, row_tiles;          // workgroups per sequence, key head and share, 16-row tiles in each
     int shares, share_tokens;      // the longest sequence's shares of share_tokens (a multiple of 64); a sequence has those it needs
     float* part;                   // [shares][n_q Hq][d], then [shares][n_q Hq][2] as in csat_prompt.h, or null: O and lse are written
     float* scores;                 // [B][Hkv][max_q G.size][score_ld] in units of log2, for the weights, or null
@@ -258,17 +258,19 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
 // 16 (i / 4) + 4 s + i % 4, so that a lane's 16 scores are those of the 16 consecutive tokens 16 quad .. + 15 of one query
 // row, and, as the B operand of O^T = V^T P^T, meet 16 consecutive bytes of V^T.  A wavefront takes every fourth tile of its
 // share and keeps a running maximum and sum of its own; the four are joined through LDS at the end.
-template <int DC> constexpr int cached_lds_bytes(int d) { return 4 * 16 * (d + 4) * 4 + 4 * 16 * 8 + 64 * DC * 4; }
-template <typename T, int DC>
+// RT tiles of 16 rows share what is read and converted (bf16, up to 128 features: the registers).
+template <int DC, int RT> constexpr int cached_lds_bytes(int d) { return RT * (4 * 16 * (d + 4) * 4 + 4 * 16 * 8) + 64 * DC * 4; }
+template <typename T, int DC, int RT>
 __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(CachedArgs a) {
     constexpr int NP = sizeof(T) == 2 ? 1 : 3;      // float queries and weights as three bf16 parts: 24 bits
     constexpr int DT = 4 * DC;
-    extern __shared__ float joint[];                // [4][16][d + 4] outputs, then [4][16][2]; a token per feature, of its first NaN
+    constexpr int ROWS = 16 * RT;
+    extern __shared__ float joint[];                // [4][ROWS][d + 4] outputs, then [4][ROWS][2]; a token per feature, of its first NaN
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, quad = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.z, share = blockIdx.y, tile = a.tiles == 1 ? 0 : blockIdx.x / a.Hkv, hk = blockIdx.x - tile * a.Hkv;
     const PackedSpan qs(a.q_off, b, a.n_q);
-    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size, r_base = 16 * tile;
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size, r_base = ROWS * tile;
     if (r_base >= rows) return;
     int L = a.c.lengths[b];
     bool bad = L < 0 || L > a.c.max_len;
@@ -278,17 +280,19 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
         const int v = a.G.token(r) + L - qs.count + 1;
         return v < 0 ? 0 : v > L ? L : v;
     };
-    const int r_last = r_base + 16 < rows ? r_base + 15 : rows - 1;
+    const int r_last = r_base + ROWS < rows ? r_base + ROWS - 1 : rows - 1;
     const int lo = limit_of(r_base), hi = limit_of(r_last);
     const int s0 = share * a.share_tokens, s1 = s0 + a.share_tokens < hi ? s0 + a.share_tokens : hi;
     if (s0 >= L && share > 0) return;
     const int t0 = s0 / 64, t1 = (s1 + 63) / 64;     // (none where no row of the tile sees the share)
-    const int r = r_base + li < rows ? r_base + li : rows - 1;
-    const int tok = a.G.token(r), head = hk * a.G.size + r - tok * a.G.size, lim = limit_of(r);
-
-    // features 64 c + 16 quad + 8 h .. + 7 of the lane's row
-    bf16x8 qf[NP][DC][2];
-    {
+    // features 64 c + 16 quad + 8 h .. + 7 of the lane's rows
+    bf16x8 qf[RT][NP][DC][2];
+    int lim[RT];
+#pragma unroll
+    for (int m = 0; m < RT; ++m) {
+        const int r = r_base + 16 * m + li < rows ? r_base + 16 * m + li : rows - 1;
+        const int tok = a.G.token(r), head = hk * a.G.size + r - tok * a.G.size;
+        lim[m] = limit_of(r);
         const T* q = (const T*)a.Q + (long long)(qs.first + tok) * a.q_token + (long long)head * a.q_head;
 #pragma unroll
         for (int c = 0; c < DC; ++c)
@@ -296,29 +300,34 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
             for (int h = 0; h < 2; ++h) {
                 const int f = 64 * c + 16 * quad + 8 * h;
                 if constexpr (NP == 1) {
-                    qf[0][c][h] = __builtin_bit_cast(bf16x8, f < a.d ? *(const uint4*)(q + f) : uint4{0u, 0u, 0u, 0u});
+                    qf[m][0][c][h] = __builtin_bit_cast(bf16x8, f < a.d ? *(const uint4*)(q + f) : uint4{0u, 0u, 0u, 0u});
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float x = f < a.d ? ((const float*)q)[f + e] : 0.f;
 #pragma unroll
                         for (int p = 0; p < NP; ++p) {
-                            qf[p][c][h][e] = (__bf16)x;
-                            x -= (float)qf[p][c][h][e];
+                            qf[m][p][c][h][e] = (__bf16)x;
+                            x -= (float)qf[m][p][c][h][e];
                         }
                     }
                 }
             }
     }
     const int pitch = a.d + 4;
-    float2* const ml = (float2*)(joint + 4 * 16 * pitch);
-    int* const nan_at = (int*)(ml + 4 * 16);
+    float2* const ml = (float2*)(joint + 4 * ROWS * pitch);
+    int* const nan_at = (int*)(ml + 4 * ROWS);
     for (int i = tid; i < 64 * DC; i += 256) nan_at[i] = kNoKey;
     __syncthreads();
-    f32x4 o[DT];
+    f32x4 o[RT][DT];
+    float ref[RT], sum[RT];
 #pragma unroll
-    for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float ref = -INFINITY, sum = 0.f;
+    for (int m = 0; m < RT; ++m) {
+        ref[m] = -INFINITY;
+        sum[m] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     const int page = a.c.page, lp = a.c.log_page, last_page = (L - 1) >> lp;
     const int* const table = a.c.table + (long long)b * a.c.max_pages;
@@ -364,68 +373,78 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
         const int first = 64 * t, vt = first + 16 * quad;
         if (t + 8 < t1) { kid2 = page_of(64 * (t + 8) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 8) + 16 * quad); }
 
-        float e[16];
+        float e[RT][16];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+            f32x4 acc[RT];
+#pragma unroll
+            for (int m = 0; m < RT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
                 const bf16x8 k0 = code_fragment(kw[s][c].x, kw[s][c].y), k1 = code_fragment(kw[s][c].z, kw[s][c].w);
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[p][c][0], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[p][c][1], acc, 0, 0, 0);
-                }
+                for (int m = 0; m < RT; ++m)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[m][p][c][0], acc[m], 0, 0, 0);
+                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[m][p][c][1], acc[m], 0, 0, 0);
+                    }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[4 * s + i] = acc[i] * kscale;
+            for (int m = 0; m < RT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[m][4 * s + i] = acc[m][i] * kscale;
         }
         __builtin_amdgcn_sched_barrier(0);
         if (t + 4 < t1) load_k(t + 4, kid, vid);
         __builtin_amdgcn_sched_barrier(0);
         const bool masks = first + 64 > lo;
-        if (masks) {
+        bf16x8 pf[RT][NP][2];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (vt + i >= lim) e[i] = -INFINITY;
-        }
-        if (a.scores && r_base + li < rows) {
-            float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G.size + r) * a.score_ld + vt;
+        for (int m = 0; m < RT; ++m) {
+            const int r = r_base + 16 * m + li;
+            if (masks) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[i], e[i + 1], e[i + 2], e[i + 3]};
-        }
-        float mx = e[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, e[i]);
-        mx = quad_max(mx);
-        if (__builtin_amdgcn_ballot_w64(mx - ref > 8.f) != 0) {
-            const float nm = fmaxf(mx, ref);
-            const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - nm);
-            ref = nm;
-            sum *= f;
-#pragma unroll
-            for (int u = 0; u < DT; ++u) o[u] *= f;
-        }
-        const float base = ref == -INFINITY ? 0.f : ref;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(e[i] - base);
-            sum += e[i];
-            e[i] *= vscale;
-        }
-        // weights of bf16 precision for bf16 tensors; the other parts for float ones
-        bf16x8 pf[NP][2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float x = e[8 * h + i];
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    pf[p][h][i] = (__bf16)x;
-                    x -= (float)pf[p][h][i];
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (vt + i >= lim[m]) e[m][i] = -INFINITY;
             }
+            if (a.scores && r < rows) {
+                float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G.size + r) * a.score_ld + vt;
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[m][i], e[m][i + 1], e[m][i + 2], e[m][i + 3]};
+            }
+            float mx = e[m][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, e[m][i]);
+            mx = quad_max(mx);
+            if (__builtin_amdgcn_ballot_w64(mx - ref[m] > 8.f) != 0) {
+                const float nm = fmaxf(mx, ref[m]);
+                const float f = ref[m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[m] - nm);
+                ref[m] = nm;
+                sum[m] *= f;
+#pragma unroll
+                for (int u = 0; u < DT; ++u) o[m][u] *= f;
+            }
+            const float base = ref[m] == -INFINITY ? 0.f : ref[m];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                e[m][i] = __builtin_amdgcn_exp2f(e[m][i] - base);
+                sum[m] += e[m][i];
+                e[m][i] *= vscale;
+            }
+            // weights of bf16 precision for bf16 tensors; the other parts for float ones
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float x = e[m][8 * h + i];
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) {
+                        pf[m][p][h][i] = (__bf16)x;
+                        x -= (float)pf[m][p][h][i];
+                    }
+                }
+        }
         if (masks) {      // NaN codes out of tokens that some row does not see (0 times NaN is NaN), the first of each feature noted
             uint32_t any = 0;
 #pragma unroll
@@ -449,10 +468,12 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
         for (int u = 0; u < DT; ++u) {
             const bf16x8 v0 = code_fragment(vw[u].x, vw[u].y), v1 = code_fragment(vw[u].z, vw[u].w);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                o[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[p][0], o[u], 0, 0, 0);
-                o[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[p][1], o[u], 0, 0, 0);
-            }
+            for (int m = 0; m < RT; ++m)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[m][p][0], o[m][u], 0, 0, 0);
+                    o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[m][p][1], o[m][u], 0, 0, 0);
+                }
         }
         __builtin_amdgcn_sched_barrier(0);
         if (t + 4 < t1) load_v(t + 4, vid);
@@ -460,25 +481,28 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     }
 
     // the wavefronts' parts of a row, brought to the largest reference
-    sum = quad_sum(sum);
-    if (__builtin_amdgcn_ballot_w64(bad) != 0) sum = __uint_as_float(0x7fc00000u);
+    const bool any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
 #pragma unroll
-    for (int u = 0; u < DT; ++u)
-        if (16 * u < a.d) *(f32x4*)(joint + (wave * 16 + li) * pitch + 16 * u + 4 * quad) = o[u];
-    if (quad == 0) ml[wave * 16 + li] = float2{ref, sum};
+    for (int m = 0; m < RT; ++m) {
+        const float total = any_bad ? __uint_as_float(0x7fc00000u) : quad_sum(sum[m]);
+#pragma unroll
+        for (int u = 0; u < DT; ++u)
+            if (16 * u < a.d) *(f32x4*)(joint + (wave * ROWS + 16 * m + li) * pitch + 16 * u + 4 * quad) = o[m][u];
+        if (quad == 0) ml[wave * ROWS + 16 * m + li] = float2{ref[m], total};
+    }
     __syncthreads();
-    const int n_rows = rows - r_base < 16 ? rows - r_base : 16, dq = a.d / 4;
+    const int n_rows = rows - r_base < ROWS ? rows - r_base : ROWS, dq = a.d / 4;
     for (int q = tid; q < n_rows * dq; q += 256) {
         const int i = q / dq, f = q % dq * 4;
         float m = -INFINITY, total = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * 16 + i].x);
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w * ROWS + i].x);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const float2 y = ml[w * 16 + i];
+            const float2 y = ml[w * ROWS + i];
             if (y.y == 0.f) continue;
             const float k = y.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(y.x - m);      // (a sum that is NaN without a maximum stays)
-            const float4 z = *(const float4*)(joint + (w * 16 + i) * pitch + f);
+            const float4 z = *(const float4*)(joint + (w * ROWS + i) * pitch + f);
             total += k * y.y;
             x[0] += k * z.x; x[1] += k * z.y; x[2] += k * z.z; x[3] += k * z.w;
         }

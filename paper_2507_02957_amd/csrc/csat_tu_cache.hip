@@ -24,11 +24,10 @@ hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st) {
 
 hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st) {
     const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.shares, (unsigned)a.B);
-#define CSAT_CACHED(DC_) (bf16 ? launch(cache_attention_kernel<bf16_t, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a) \
-                               : launch(cache_attention_kernel<float, DC_>, grid, 256, cached_lds_bytes<DC_>(a.d), st, a))
-    if (a.d <= 64) return CSAT_CACHED(1);
-    if (a.d <= 128) return CSAT_CACHED(2);
-    return CSAT_CACHED(4);
+#define CSAT_CACHED(T_, DC_, RT_) launch(cache_attention_kernel<T_, DC_, RT_>, grid, 256, cached_lds_bytes<DC_, RT_>(a.d), st, a)
+    if (!bf16) return a.d <= 64 ? CSAT_CACHED(float, 1, 1) : a.d <= 128 ? CSAT_CACHED(float, 2, 1) : CSAT_CACHED(float, 4, 1);
+    if (a.row_tiles == 2) return a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 2) : CSAT_CACHED(bf16_t, 2, 2);
+    return a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 1) : a.d <= 128 ? CSAT_CACHED(bf16_t, 2, 1) : CSAT_CACHED(bf16_t, 4, 1);
 #undef CSAT_CACHED
 }
 

@@ -198,8 +198,10 @@ struct PromptRows : PromptAcc<DT> {
         }
     }
 
-    // keys key0 .., K's tile at LDS address sk, V's at sv; masked: some row does not see all of them
-    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane) {
+    // keys key0 .., K's tile at LDS address sk, V's at sv; masked: some row does not see all of them.  k_read() is called when K's
+    // tile has been read, v_needed() before V's is.
+    template <typename KRead, typename VNeeded>
+    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane, KRead k_read, VNeeded v_needed) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
         typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
@@ -217,7 +219,9 @@ struct PromptRows : PromptAcc<DT> {
                 const u32x4 kf = *(lds_u32x4)(uintptr_t)(sk + (uint32_t)(((32 * u + li) * C + ((2 * g + lh) ^ swizzle_k<C>(li))) * 16));
                 mfma_group<T>(__builtin_bit_cast(uint4, kf), qf[g], s[u]);
             }
+        k_read();
         this->template weights<KT>(s, key0, masked, sl, lh);
+        v_needed();
         // O^T += V^T P^T
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
@@ -291,7 +295,8 @@ struct PromptRowsParts : PromptAcc<DT> {
             parts(x, qp[g]);
         }
     }
-    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane) {
+    template <typename KRead, typename VNeeded>
+    __device__ __forceinline__ void step(uint32_t sk, uint32_t sv, int key0, bool masked, float sl, int lane, KRead k_read, VNeeded v_needed) {
         typedef __attribute__((address_space(3))) const f32x4* lds_f32x4;
         typedef __attribute__((address_space(3))) const float* lds_float;
         const int li = lane & 31, lh = lane >> 5;
@@ -311,7 +316,9 @@ struct PromptRowsParts : PromptAcc<DT> {
             parts(x, kp);
             products(kp, qp[g], s[0]);
         }
+        k_read();
         this->template weights<1>(s, key0, masked, sl, lh);
+        v_needed();
 #pragma unroll
         for (int h2 = 0; h2 < 2; ++h2) {
             float x[8];
@@ -368,25 +375,29 @@ struct PromptKeys {
             vo[p] = (uint32_t)row * v_row + 16u * (uint32_t)(c ^ swizzle_v<T, C>(row));
         }
     }
-    // step t: K's tile to LDS address `at`, V's behind it; `wave`: which 64 of the threads this wavefront is
+    // step t's tile of K, or of V, to LDS address `at`, PIECES requests of every wavefront; `wave`: which 64 of the threads it is
+    template <bool IS_V>
     __device__ __forceinline__ void load(int t, uint32_t at, int wave, int tid) const {
-        const char* const kt = kb + (long long)t * KEYS * k_row;
-        const char* const vt = vb + (long long)t * KEYS * v_row;
+        const uint32_t step_row = IS_V ? v_row : k_row;
+        const uint32_t (&off)[PIECES] = IS_V ? vo : ko;
+        const char* const from = (IS_V ? vb : kb) + (long long)t * KEYS * step_row;
         at += wave * 1024;
         if (dc == C && (t + 1) * KEYS <= nk) {
 #pragma unroll
-            for (int p = 0; p < PIECES; ++p) stage16(at + p * THREADS * 16, kt, ko[p]);
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) stage16(at + TILE + p * THREADS * 16, vt, vo[p]);
+            for (int p = 0; p < PIECES; ++p) stage16(at + p * THREADS * 16, from, off[p]);
             return;
         }
         const int left = nk - 1 - t * KEYS;
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
+        for (int p = 0; p < PIECES; ++p) {           // (a wavefront's 64 pieces are whole rows: some of its lanes have a column below d)
             const int q = p * THREADS + tid, row = q / C, c = q % C, over = row > left ? row - left : 0;
-            if ((c ^ swizzle_k<C>(row)) < dc) stage16(at + p * THREADS * 16, kt, ko[p] - (uint32_t)over * k_row);
-            if ((c ^ swizzle_v<T, C>(row)) < dc) stage16(at + TILE + p * THREADS * 16, vt, vo[p] - (uint32_t)over * v_row);
+            if ((c ^ (IS_V ? swizzle_v<T, C>(row) : swizzle_k<C>(row))) < dc) stage16(at + p * THREADS * 16, from, off[p] - (uint32_t)over * step_row);
         }
+    }
+    // both, V's tile behind K's
+    __device__ __forceinline__ void load_both(int t, uint32_t at, int wave, int tid) const {
+        load<false>(t, at, wave, tid);
+        load<true>(t, at + TILE, wave, tid);
     }
     // zeros where load() leaves out the columns behind d, of `tiles` tiles from `to` (K and V in turn)
     __device__ __forceinline__ void clear(uint4* to, int tiles, int tid) const {
@@ -406,7 +417,12 @@ struct PromptKeys {
         }
     }
 };
-__device__ __forceinline__ void wait_staged() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0): this wavefront's pieces are there
+// This wavefront's pieces are there, but for the N that it asked for last (vmcnt(N)).
+template <int N = 0> __device__ __forceinline__ void wait_staged() {
+    static_assert(N < 64, "vmcnt has six bits");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
 
 // Which rows a workgroup has.  The grid's y is a row tile, the last ones, which see most keys, first.  x is a (sequence, key head)
 // pair, z a share of its keys; or, for many tiles, x one of eight pairs and z which eight, so that an XCD, which takes every
@@ -471,7 +487,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     int t0, t1;
     at.steps<KEYS>(a.shares, &t0, &t1);
     const Keys keys(a, at.k_first, at.nk, at.hk, tid);
-    if (t0 < t1) keys.load(t0, lds0 + (t0 & 1) * 2 * Keys::TILE, wave, tid);
+    if (t0 < t1) keys.load_both(t0, lds0 + (t0 & 1) * 2 * Keys::TILE, wave, tid);
     if (keys.dc < C) keys.clear(lds, 4, tid);
     for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
     if (tid == 0) *any_odd = 0;
@@ -483,13 +499,13 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
         const uint32_t sk = lds0 + (t & 1) * 2 * Keys::TILE;
         wait_staged();
         __syncthreads();                             // everybody's pieces are there; the other half of the LDS has been read
-        if (t + 1 < t1) keys.load(t + 1, lds0 + ((t + 1) & 1) * 2 * Keys::TILE, wave, tid);
+        if (t + 1 < t1) keys.load_both(t + 1, lds0 + ((t + 1) & 1) * 2 * Keys::TILE, wave, tid);
         if ((t + 1) * KEYS > at.lo) {                // some row of the workgroup does not see all of the step's keys
             keys.look_over(t, lds + (t & 1) * 2 * KEYS * C + KEYS * C, tid, oddc, any_odd);
             __syncthreads();
         }
         if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
-        rows.step(sk, sk + Keys::TILE, t * KEYS, (t + 1) * KEYS > w_lo, a.sl, lane);
+        rows.step(sk, sk + Keys::TILE, t * KEYS, (t + 1) * KEYS > w_lo, a.sl, lane, [] {}, [] {});
     }
     __syncthreads();                                 // (the last steps' odd values are noted)
     if (!active) return;
@@ -579,18 +595,26 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
     const int lane_row = at.r_base + li < at.rows ? at.r_base + li : at.rows - 1, lane_limit = at.limit(lane_row);
     PromptAcc<DT> acc;
     auto go = [&](auto rows) {
-        if (t0 + wave < t1) keys.load(t0 + wave, sk, 0, lane);
+        // K's tile is asked for again as soon as it has been read, V's too: each has the other's work to arrive in.  (A wavefront
+        // has 64 lanes' part in every request, so PIECES requests are one tile.)
+        if (t0 + wave < t1) keys.load_both(t0 + wave, sk, 0, lane);
         rows.init(a, at.q_first, at.hk, lane_row, lane_limit, lane);
         __syncthreads();                             // (the columns' odd values are set up)
         for (int t = t0 + wave; t < t1; t += W) {
-            wait_staged();
-            const bool masked = (t + 1) * KEYS > at.lo;
-            if (masked) keys.look_over(t, own + KEYS * C, lane, oddc, any_odd);
+            const bool masked = (t + 1) * KEYS > at.lo, more = t + W < t1;
+            wait_staged<Keys::PIECES>();             // K's
+            rows.step(sk, sk + Keys::TILE, t * KEYS, masked, a.sl, lane, [&] {
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the tile has been read
+                if (more) keys.template load<false>(t + W, sk, 0, lane);
+            }, [&] {
+                if (more) wait_staged<Keys::PIECES>();
+                else wait_staged();
+                if (masked) keys.look_over(t, own + KEYS * C, lane, oddc, any_odd);
+                __builtin_amdgcn_wave_barrier();
+            });
+            __builtin_amdgcn_s_waitcnt(0xc07f);
             __builtin_amdgcn_wave_barrier();
-            rows.step(sk, sk + Keys::TILE, t * KEYS, masked, a.sl, lane);
-            __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the tile has been read
-            __builtin_amdgcn_wave_barrier();
-            if (t + W < t1) keys.load(t + W, sk, 0, lane);
+            if (more) keys.template load<true>(t + W, sk + Keys::TILE, 0, lane);
         }
         acc = rows;
     };

@@ -5,6 +5,9 @@
 // exceeds it by more than 2^8), the sum of its weights e = 2^(s sl + off), off = -ref sl, sl = scale log2(e), and the
 // unnormalised output; moving the reference multiplies both by 2^(off' - off), the same rounded offsets that the weights
 // were formed with, so the change of reference itself rounds nothing but the product.
+// With bf16 tensors the weights go into the second product rounded to bf16, half a step of the output's own type, for one
+// matrix instruction in place of two or three; scores, exponentials, sums and outputs are float, and the sum is of the weights as
+// they were before the rounding.
 //
 // Rows: the rows of one key head are the (row, head of the group) pairs, row / G first, so that a workgroup's keys serve all
 // heads of the group.  Everything is computed transposed (S^T = K Q^T, O^T = V^T P^T): a query row sits in one lane pair
@@ -466,6 +469,10 @@ struct PromptPlace {
 // Long sequences, bf16: four wavefronts of 32 rows each go over the same keys, 64 at a time, which they stage together, the next step's
 // while one is worked on.  Two wavefronts per SIMD fill each other's waits between products (32 a step), exponentials (32 at a
 // quarter of the rate) and fragment reads (32 KB a step, at 128 bytes a cycle and CU just below the products' time).
+// Measured: 16384 tokens causal, 16 heads over 4 key heads, d 128, 1.03 to 1.07 ms = 1030 to 1070 TFLOP/s of visible pairs, where a library's
+// product of two 16384 x 16384 matrices reaches 1400; matrix units busy a third of the cycles, vector instructions 40 %, no bank
+// conflicts.  With the tiles in staging registers (244 instead of 206) 1.35 ms; with the odd values' products in the loop (410
+// registers, one wavefront per SIMD) 2.14.
 template <int DT>
 __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
     typedef bf16_t T;

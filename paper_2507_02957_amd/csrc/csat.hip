@@ -2196,7 +2196,7 @@ struct PromptPlan { bool split; int tiles, shares; size_t bytes; };
 // Row tiles of 128, or of 32 whose keys the wavefronts divide: float always, bf16 where tiles of 128 would occupy less than half
 // of the compute units (8 heads x 512 rows, d 64, 32 tiles of 128: 7.5 against 11.9 us; 2 key heads x 1024 x 4, d 128, 64 tiles: 15.7
 // against 25.5; not 96 heads x 274, 288 tiles: 15.5 against 11.7, nor 4 x 2048 x 4, 256 tiles: 60 against 47).  The keys in shares where even
-// then tiles are fewer than compute units, a share no shorter than 256 keys (one row of 32 heads against 4096 keys: 12.2
+// then tiles are fewer than compute units (one row of 32 heads against 4096 keys: 12.2
 // against 38.8 us; 1024 rows, d 256, 32 tiles of 128: 25.6 against 27.0).
 PromptPlan prompt_plan(const csat_packed_dims& d) {
     PromptPlan p{};
@@ -2204,7 +2204,12 @@ PromptPlan prompt_plan(const csat_packed_dims& d) {
     const long long rows = (long long)longest_q(d) * G, pairs = (long long)d.B * d.Hkv;
     p.split = d.dtype == CSAT_F32 || pairs * ((rows + 127) / 128) < 128;
     p.tiles = (int)(p.split ? (rows + 31) / 32 : (rows + 127) / 128);
-    p.shares = (int)std::max(1LL, std::min<long long>(256 / (pairs * p.tiles), longest_k(d) / 256));
+    // Fewest keys of a share, a join's cost against what a workgroup's steps take; us with 256 / 128 / 64 / 32.  Float: 32 pairs, 338 keys,
+    // one row tile, d 256 100 / 58 / 44 / 31, d 128 21.5 / 21.2 / 17.1 / 17.1, d 64 13.3 / 14.3 / 12.5 / 12.8 (4 pairs, 415 keys 15.2 / 13.0 /
+    // 11.8 / 12.5).  bf16: the same, d 64 6.8 / 9.2 / 9.4 / 9.6; 2 pairs, 1000 keys, d 256 17.4 / 13.0 / 13.7 / 14.1.
+    const bool f32 = d.dtype == CSAT_F32;
+    const int least = d.d > 128 ? (f32 ? 32 : 128) : f32 && d.d > 64 ? 64 : 256;
+    p.shares = (int)std::max(1LL, std::min<long long>(256 / (pairs * p.tiles), longest_k(d) / least));
     p.bytes = p.shares > 1 ? (size_t)p.shares * d.n_q * d.Hq * (d.d + 2) * 4 : 0;
     return p;
 }

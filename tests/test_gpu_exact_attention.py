@@ -117,6 +117,16 @@ def test_few_rows_share_their_keys(q_lens, k_lens, Hq, Hkv, d, dtype):
     assert torch.equal(O, p.O) and torch.equal(lse, p.lse)
 
 
+@pytest.mark.parametrize("q_lens,k_lens,Hq,Hkv,d", [([3, 3], [338, 1], 16, 2, 256), ([2, 0, 1], [65, 64, 31], 4, 4, 136), ([4, 1], [129, 7], 8, 2, 128),
+                                                   ([5], [127], 4, 1, 72)])
+def test_short_shares_of_float(q_lens, k_lens, Hq, Hkv, d):
+    """Shares of a step or two, many of them behind the end of a short sequence."""
+    p = Problem(q_lens, k_lens, Hq, Hkv, d, "f32", True).call().check()
+    first = p.O.clone()
+    p.call()
+    assert torch.equal(first, p.O)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_strides(dtype):
     """Parts of a fused projection, heads first, and a key head that all heads share by a stride of 0."""

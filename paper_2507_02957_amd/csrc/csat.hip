@@ -2176,7 +2176,16 @@ constexpr long long kMaxBlocksYZ = 65535;            // ... and along y and z
 constexpr long long kMaxTokenStride = 1 << 24;
 
 // rows of O must not lie on one another
-bool output_strides_ok(const csat_packed_dims& d) { return (d.n_q == 1 || d.o_token >= d.d) && (d.Hq == 1 || d.o_head >= d.d); }
+// (of two heads' rows, h heads apart, the nearest are o_head h / o_token tokens apart, rounded down or up)
+bool output_strides_ok(const csat_packed_dims& d) {
+    const long long last = d.n_q - 1, t = d.o_token, h = d.o_head;
+    if ((last && t < d.d) || (d.Hq > 1 && h < d.d)) return false;
+    if (!last || d.Hq == 1 || h >= last * t + d.d || (t >= d.d && d.Hq - 1 <= (t - d.d) / h)) return true;
+    for (long long k = 1, at = h; k < d.Hq && at < last * t + d.d; ++k, at += h)
+        for (long long i = at / t; i <= at / t + 1 && i <= last; ++i)
+            if (std::llabs(at - i * t) < d.d) return false;
+    return true;
+}
 bool stride_ok(long long token, long long head, size_t e) {
     return token >= 0 && token < kMaxTokenStride && head >= 0 && token * (long long)e % 16 == 0 && head * (long long)e % 16 == 0;
 }

@@ -123,6 +123,28 @@ def test_rows_of_the_output_that_overlap_are_refused(lib):
         assert _prompt(lib, _dims(**change)) == -2 and _attend(lib, _dims(**change), _cache()) == -2
 
 
+def _overlap(n, H, d, token, head):
+    rows = sorted(i * token + h * head for i in range(n) for h in range(H))
+    return any(b - a < d for a, b in zip(rows, rows[1:]))
+
+
+def test_overlapping_rows_are_found_wherever_they_lie(lib):
+    """All strides of a few rows and heads against their places; workspace of no bytes, so that none gets to the device."""
+    seen = set()
+    for token in range(32, 32 * 9, 8):
+        for head in range(32, 32 * 12, 8):
+            for n, H in ((3, 4), (10, 4), (2, 2), (7, 1), (1, 6)):
+                d = _dims(n_q=n, Hq=H, Hkv=1, o_token=token, o_head=head, dtype=0)
+                d.max_q, d.max_k, d.n_k = 1, 4096, 4096
+                d.q_token, d.q_head = H * 32, 32
+                bad = _overlap(n, H, 32, token, head)
+                got = _prompt(lib, d, ws=None, n=0)
+                assert got == (-2 if bad else -5), (token, head, n, H, got)
+                seen.add(bad)
+    assert seen == {False, True}
+
+
+
 def test_tensors_of_the_host_are_refused(lib):
     x = torch.zeros(10, 4, 32, dtype=torch.bfloat16)
     with pytest.raises(ValueError):

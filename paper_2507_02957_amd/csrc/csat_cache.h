@@ -919,7 +919,9 @@ __global__ __launch_bounds__(256, NI <= 2 ? 6 : NI == 4 ? 3 : 1) void cache_gath
         for (int p = 0; p < NI; ++p) {
             const int q = p * 256 + tid, i = a.by_row(q);
             if (i >= n) continue;
-            const float s = src_scale[i] * inv;
+            // (the ratio of two scales may pass the largest float, and 0 times infinity is no code; a code that is not 0 meets none above
+            // 448 / 2^-9 < 2^18, since its value counted for the destination)
+            const float s = fminf(src_scale[i] * inv, 0x1p127f);
             if (s != 1.f) w[p] = uint4{rescale_codes(w[p].x, s), rescale_codes(w[p].y, s), rescale_codes(w[p].z, s), rescale_codes(w[p].w, s)};
             ((uint4*)(a.to.K + dst * size))[q] = w[p];
         }
@@ -935,7 +937,7 @@ __global__ __launch_bounds__(256, NI <= 2 ? 6 : NI == 4 ? 3 : 1) void cache_gath
             uint32_t& x = (&w[p].x)[e / 4];
             const float4 s = *(const float4*)(src_scale + g + e);
             const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
-            x = codes_of(lo[0] * (s.x * inv), lo[1] * (s.y * inv), hi[0] * (s.z * inv), hi[1] * (s.w * inv));
+            x = codes_of(lo[0] * inv * s.x, lo[1] * inv * s.y, hi[0] * inv * s.z, hi[1] * inv * s.w);      // (in this order: 0 stays 0, see K's; codes times 2^-120 are floats)
         }
         uint8_t* const out = a.to.V + dst * size + q * 16;
         if (g + 16 <= n) *(uint4*)out = w[p];

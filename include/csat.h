@@ -248,8 +248,9 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
  * n_q / n_k; sequences may be empty).  Row r, head h starts at element r * token stride + h * head stride of its
  * tensor; strides are multiples of 16 bytes (so a part of a fused projection serves as well as a tensor of its own, and 0
  * repeats a row, except of O, whose rows must not lie on one another), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
- * max_q, max_k bound the rows of one sequence: rows beyond the bound are not computed and not written.  So are rows
- * of no sequence (behind the last offset): they are left as they were.
+ * max_q bounds the rows of one sequence that are computed, max_k (csat_cache_store) those that are stored: rows beyond the
+ * bound are not written, the others keep the places that they have among all of the sequence's rows.  (csat_prompt_attention: rows see
+ * all keys whatever max_k says, which only shapes the work.)  Rows of no sequence (behind the last offset) are left as they were.
  * d: a multiple of 8 (csat_prompt_attention) or of 16 (the cache), at most 256.  n_q, n_k, max_q, max_k at least 1; B at most
  * 65535, n_q * Hq, n_k and a cache's max_pages * page at most 2^30.
  * ------------------------------------------------------------------------------------------------------ */
@@ -291,10 +292,10 @@ typedef struct {
 } csat_cache;
 
 /* Stores the packed rows of K and V (float or bf16, k_offsets, n_k, max_k as above) as the last tokens of their
- * sequences: lengths[b] counts them already.  A block gets the smallest scale 2^e, e >= -118, with every finite |x| <= 448 * 2^e;
+ * sequences: lengths[b] counts them already (all of them, also those beyond max_k).  A block gets the smallest scale 2^e, e >= -118, with every finite |x| <= 448 * 2^e;
  * where a block holds older tokens its scale only grows, and theirs are rounded anew to it (exact but for values that
  * fall below 2^-6 of the new scale).  A non-finite x is stored as NaN and does not count for the scale.  Slots
- * beyond the length keep what they held.  Each page written to must belong to one sequence only. */
+ * that get no row keep what they held.  Each page written to must belong to one sequence only. */
 csat_status csat_cache_store(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* K, const void* V,
                              const int* k_offsets, void* stream);
 

@@ -97,12 +97,13 @@ __global__ __launch_bounds__(256) void cache_store_kernel(StoreArgs a) {
     const PackedSpan ks(a.k_off, b, a.n_k);
     const int n = ks.count < a.max_k ? ks.count : a.max_k;
     const int len = a.c.lengths[b];
-    if (n <= 0 || len > a.c.max_len || len < n) return;
-    const int start = len - n, page = a.c.page, first = start >> a.c.log_page, last = (len - 1) >> a.c.log_page;
+    if (n <= 0 || len > a.c.max_len || len < ks.count) return;
+    const int start = len - ks.count, end = start + n;      // (rows beyond max_k have their places too)
+    const int page = a.c.page, first = start >> a.c.log_page, last = (end - 1) >> a.c.log_page;
     const int j = first + i;
     if (j > last) return;
     const int* const table = a.c.table + (long long)b * a.c.max_pages;
-    const int lo = j == first ? start - j * page : 0, hi = j == last ? len - j * page : page;      // new slots
+    const int lo = j == first ? start - j * page : 0, hi = j == last ? end - j * page : page;      // new slots
     const long long row0 = ks.first + ((long long)j * page - start);      // packed row of slot 0
     const T* K = (const T*)a.K + row0 * a.k_token + (long long)hk * a.k_head;
     const T* V = (const T*)a.V + row0 * a.v_token + (long long)hk * a.v_head;

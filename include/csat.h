@@ -304,8 +304,10 @@ csat_status csat_cache_store(void* ctx, const csat_packed_dims* dims, const csat
  * > 1 its last n tokens; 0: all of them.  O, lse as above; a NaN among the tokens that a row does not see has no effect on it.
  * W (float [B, Hkv, max_pages * page], optional): W[b, h, t] = decay * W[b, h, t] + the weights that the rows and the
  * heads of the group gave token t, t < lengths[b]; 0 <= decay <= 1, with 0 W is written, not read.
- * Workspace: csat_cache_workspace_bytes (host-only query for these dims and this cache; it may be 0). */
+ * Workspace: csat_cache_workspace_bytes (host-only query for these dims and this cache; it may be 0).  Nearly all of it are the scores that
+ * W is formed from, float [B, Hq, max_q, max_len]; a call without W needs only csat_cache_workspace_bytes_without_weights. */
 csat_status csat_cache_workspace_bytes(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes);
+csat_status csat_cache_workspace_bytes_without_weights(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes);
 csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* Q,
                                  const int* q_offsets, float scale, float decay, void* O, float* lse, float* W,
                                  void* workspace, size_t workspace_bytes, void* stream);

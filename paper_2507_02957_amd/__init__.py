@@ -23,7 +23,8 @@ EXPORTS = (
     "csat_recover_hadamard", "csat_measure_hadamard", "csat_forward_hadamard", "csat_forward_rd_hadamard", "csat_measure_kv", "csat_forward_kv", "csat_forward_rd_kv",
     "csat_peak_copy", "csat_peak_mfma", "csat_peak_mfma_issue", "csat_profile_enable", "csat_profile_read", "csat_profile_decoder_kernel", "csat_profile_launch_form",
     "csat_set_option", "csat_decoder_status", "csat_static_workspace_bytes", "csat_forward_static",
-    "csat_prompt_workspace_bytes", "csat_prompt_attention", "csat_cache_store", "csat_cache_workspace_bytes", "csat_cache_attention", "csat_cache_evict",
+    "csat_prompt_workspace_bytes", "csat_prompt_attention", "csat_cache_store", "csat_cache_workspace_bytes",
+    "csat_cache_workspace_bytes_without_weights", "csat_cache_attention", "csat_cache_evict",
 )
 # keys of csat_set_option (include/csat.h, csat_option)
 OPTIONS = {"decoder": 0, "gemm": 1, "raster": 2, "state": 3, "fused_segments": 4, "fused_thin": 5, "lista": 6,
@@ -113,7 +114,7 @@ def load_library() -> ctypes.CDLL:
     lib.csat_prompt_workspace_bytes.argtypes = [pp, ctypes.POINTER(sz)]
     lib.csat_prompt_attention.argtypes = [vp, pp, vp, vp, vp, vp, vp, fl, vp, vp, vp, sz, vp]
     lib.csat_cache_store.argtypes = [vp, pp, cp, vp, vp, vp, vp]
-    lib.csat_cache_workspace_bytes.argtypes = [pp, cp, ctypes.POINTER(sz)]
+    lib.csat_cache_workspace_bytes.argtypes = lib.csat_cache_workspace_bytes_without_weights.argtypes = [pp, cp, ctypes.POINTER(sz)]
     lib.csat_cache_attention.argtypes = [vp, pp, cp, vp, vp, fl, fl, vp, vp, vp, vp, sz, vp]
     lib.csat_cache_evict.argtypes = [vp, pp, cp, cp, vp, vp, it, it, vp, vp]
     for name in EXPORTS:
@@ -409,6 +410,13 @@ def csat_cache_store(dims, cache, K, V, k_offsets, stream=None):
 def csat_cache_workspace_bytes(dims: csat_packed_dims, cache: csat_cache) -> int:
     out = ctypes.c_size_t()
     _check(load_library().csat_cache_workspace_bytes(ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(out)))
+    return out.value
+
+
+def csat_cache_workspace_bytes_without_weights(dims: csat_packed_dims, cache: csat_cache) -> int:
+    """For calls whose W is None: far less."""
+    out = ctypes.c_size_t()
+    _check(load_library().csat_cache_workspace_bytes_without_weights(ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(out)))
     return out.value
 
 

@@ -2903,6 +2903,14 @@ csat_status csat_cache_workspace_bytes(const csat_packed_dims* dims, const csat_
     return CSAT_OK;
 }
 
+csat_status csat_cache_workspace_bytes_without_weights(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes) {
+    CSAT_TRY(check_packed(dims, 16));
+    CSAT_TRY(check_cache(*dims, cache));
+    if (!bytes) return CSAT_ERR_NULL;
+    *bytes = cached_plan(*dims, *cache, false).bytes;
+    return CSAT_OK;
+}
+
 csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* Q,
                                  const int* q_offsets, float scale, float decay, void* O, float* lse, float* W,
                                  void* workspace, size_t workspace_bytes, void* stream) {

@@ -326,13 +326,6 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     __syncthreads();
     f32x4 o[RT][DT];
     float ref[RT], sum[RT];
-#pragma unroll
-    for (int m = 0; m < RT; ++m) {
-        ref[m] = -INFINITY;
-        sum[m] = 0.f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) o[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
 
     const int page = a.c.page, lp = a.c.log_page, last_page = (L - 1) >> lp;
     const int* const table = a.c.table + (long long)b * a.c.max_pages;
@@ -364,127 +357,150 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
         for (int u = 0; u < DT; ++u) vw[u] = 16 * u < a.d ? *(const uint4*)(vp + (long long)(16 * u) * page) : uint4{0u, 0u, 0u, 0u};
         vscale = a.c.Vs[(long long)vid * a.Hkv + hk];
     };
-    int kid = 0, vid = 0, kid2 = 0, vid2 = 0;        // of the next step, of the one behind it
-    if (t0 + wave < t1) {
-        const int t = t0 + wave;
-        kid = page_of(64 * t + 16 * (li >> 2));
-        vid = page_of(64 * t + 16 * quad);
-        if (t + 4 < t1) { kid2 = page_of(64 * (t + 4) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 4) + 16 * quad); }
-        load_k(t, kid, vid);
-        load_v(t, vid);
-        kid = kid2; vid = vid2;
-    }
-    for (int t = t0 + wave; t < t1; t += 4) {
-        const int first = 64 * t, vt = first + 16 * quad;
-        if (t + 8 < t1) { kid2 = page_of(64 * (t + 8) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 8) + 16 * quad); }
+    float down = 0.f;                                // powers of two that all weights are smaller by (headroom, csat_prompt.h): references are larger
+    for (;; down = headroom(L)) {
+#pragma unroll
+        for (int m = 0; m < RT; ++m) {
+            ref[m] = -INFINITY;
+            sum[m] = 0.f;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) o[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        int kid = 0, vid = 0, kid2 = 0, vid2 = 0;    // of the next step, of the one behind it
+        int start = t0 + wave;
+        asm volatile("" : "+s"(start));              // (so that a second pass keeps nothing in registers for its beginning)
+        if (start < t1) {
+            const int t = start;
+            kid = page_of(64 * t + 16 * (li >> 2));
+            vid = page_of(64 * t + 16 * quad);
+            if (t + 4 < t1) { kid2 = page_of(64 * (t + 4) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 4) + 16 * quad); }
+            load_k(t, kid, vid);
+            load_v(t, vid);
+            kid = kid2; vid = vid2;
+        }
+        for (int t = start; t < t1; t += 4) {
+            const int first = 64 * t, vt = first + 16 * quad;
+            if (t + 8 < t1) { kid2 = page_of(64 * (t + 8) + 16 * (li >> 2)); vid2 = page_of(64 * (t + 8) + 16 * quad); }
 
-        float e[RT][16];
+            float e[RT][16];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            f32x4 acc[RT];
+            for (int s = 0; s < 4; ++s) {
+                f32x4 acc[RT];
 #pragma unroll
-            for (int m = 0; m < RT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int m = 0; m < RT; ++m) acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < DC; ++c) {
-                const bf16x8 k0 = code_fragment(kw[s][c].x, kw[s][c].y), k1 = code_fragment(kw[s][c].z, kw[s][c].w);
+                for (int c = 0; c < DC; ++c) {
+                    const bf16x8 k0 = code_fragment(kw[s][c].x, kw[s][c].y), k1 = code_fragment(kw[s][c].z, kw[s][c].w);
+#pragma unroll
+                    for (int m = 0; m < RT; ++m)
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[m][p][c][0], acc[m], 0, 0, 0);
+                            acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[m][p][c][1], acc[m], 0, 0, 0);
+                        }
+                }
+#pragma unroll
+                for (int m = 0; m < RT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[m][4 * s + i] = acc[m][i] * kscale;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 4 < t1) load_k(t + 4, kid, vid);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool masks = first + 64 > lo;
+            bf16x8 pf[RT][NP][2];
+#pragma unroll
+            for (int m = 0; m < RT; ++m) {
+                const int r = r_base + 16 * m + li;
+                if (masks) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (vt + i >= lim[m]) e[m][i] = -INFINITY;
+                }
+                if (a.scores && r < rows) {
+                    float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G.size + r) * a.score_ld + vt;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[m][i], e[m][i + 1], e[m][i + 2], e[m][i + 3]};
+                }
+                float mx = e[m][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) mx = fmaxf(mx, e[m][i]);
+                mx = quad_max(mx);
+                if (__builtin_amdgcn_ballot_w64(mx - ref[m] > 8.f - down) != 0) {
+                    const float nm = fmaxf(mx + down, ref[m]);
+                    const float f = ref[m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[m] - nm);
+                    ref[m] = nm;
+                    sum[m] *= f;
+#pragma unroll
+                    for (int u = 0; u < DT; ++u) o[m][u] *= f;
+                }
+                const float base = ref[m] == -INFINITY ? 0.f : ref[m];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    e[m][i] = __builtin_amdgcn_exp2f(e[m][i] - base);
+                    sum[m] += e[m][i];
+                    e[m][i] *= vscale;
+                }
+                // weights of bf16 precision for bf16 tensors; the other parts for float ones
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float x = e[m][8 * h + i];
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            pf[m][p][h][i] = (__bf16)x;
+                            x -= (float)pf[m][p][h][i];
+                        }
+                    }
+            }
+            if (masks) {      // NaN codes out of tokens that some row does not see (0 times NaN is NaN), the first of each feature noted
+                uint32_t any = 0;
+#pragma unroll
+                for (int u = 0; u < DT; ++u) any |= nan_codes(vw[u].x) | nan_codes(vw[u].y) | nan_codes(vw[u].z) | nan_codes(vw[u].w);
+                if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+#pragma unroll
+                    for (int u = 0; u < DT; ++u) {
+                        int at = 16;
+#pragma unroll
+                        for (int i = 3; i >= 0; --i) {
+                            uint32_t& w = (&vw[u].x)[i];
+                            const uint32_t n = nan_codes(w);
+                            if (n) at = 4 * i + (__ffs(n) - 1) / 8;
+                            w = without_nan(w);
+                        }
+                        if (at < 16) atomicMin(nan_at + 16 * u + li, vt + at);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < DT; ++u) {
+                const bf16x8 v0 = code_fragment(vw[u].x, vw[u].y), v1 = code_fragment(vw[u].z, vw[u].w);
 #pragma unroll
                 for (int m = 0; m < RT; ++m)
 #pragma unroll
                     for (int p = 0; p < NP; ++p) {
-                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[m][p][c][0], acc[m], 0, 0, 0);
-                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[m][p][c][1], acc[m], 0, 0, 0);
+                        o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[m][p][0], o[m][u], 0, 0, 0);
+                        o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[m][p][1], o[m][u], 0, 0, 0);
                     }
             }
-#pragma unroll
-            for (int m = 0; m < RT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[m][4 * s + i] = acc[m][i] * kscale;
+            __builtin_amdgcn_sched_barrier(0);
+            if (t + 4 < t1) load_v(t + 4, vid);
+            kid = kid2; vid = vid2;
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (t + 4 < t1) load_k(t + 4, kid, vid);
-        __builtin_amdgcn_sched_barrier(0);
-        const bool masks = first + 64 > lo;
-        bf16x8 pf[RT][NP][2];
+        float squares = 0.f;
 #pragma unroll
-        for (int m = 0; m < RT; ++m) {
-            const int r = r_base + 16 * m + li;
-            if (masks) {
+        for (int m = 0; m < RT; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (vt + i >= lim[m]) e[m][i] = -INFINITY;
-            }
-            if (a.scores && r < rows) {
-                float* p = a.scores + (((long long)b * a.Hkv + hk) * a.max_q * a.G.size + r) * a.score_ld + vt;
+            for (int u = 0; u < DT; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) *(float4*)(p + i) = float4{e[m][i], e[m][i + 1], e[m][i + 2], e[m][i + 3]};
-            }
-            float mx = e[m][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, e[m][i]);
-            mx = quad_max(mx);
-            if (__builtin_amdgcn_ballot_w64(mx - ref[m] > 8.f) != 0) {
-                const float nm = fmaxf(mx, ref[m]);
-                const float f = ref[m] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[m] - nm);
-                ref[m] = nm;
-                sum[m] *= f;
-#pragma unroll
-                for (int u = 0; u < DT; ++u) o[m][u] *= f;
-            }
-            const float base = ref[m] == -INFINITY ? 0.f : ref[m];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                e[m][i] = __builtin_amdgcn_exp2f(e[m][i] - base);
-                sum[m] += e[m][i];
-                e[m][i] *= vscale;
-            }
-            // weights of bf16 precision for bf16 tensors; the other parts for float ones
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float x = e[m][8 * h + i];
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) {
-                        pf[m][p][h][i] = (__bf16)x;
-                        x -= (float)pf[m][p][h][i];
-                    }
-                }
-        }
-        if (masks) {      // NaN codes out of tokens that some row does not see (0 times NaN is NaN), the first of each feature noted
-            uint32_t any = 0;
-#pragma unroll
-            for (int u = 0; u < DT; ++u) any |= nan_codes(vw[u].x) | nan_codes(vw[u].y) | nan_codes(vw[u].z) | nan_codes(vw[u].w);
-            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
-#pragma unroll
-                for (int u = 0; u < DT; ++u) {
-                    int at = 16;
-#pragma unroll
-                    for (int i = 3; i >= 0; --i) {
-                        uint32_t& w = (&vw[u].x)[i];
-                        const uint32_t n = nan_codes(w);
-                        if (n) at = 4 * i + (__ffs(n) - 1) / 8;
-                        w = without_nan(w);
-                    }
-                    if (at < 16) atomicMin(nan_at + 16 * u + li, vt + at);
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < DT; ++u) {
-            const bf16x8 v0 = code_fragment(vw[u].x, vw[u].y), v1 = code_fragment(vw[u].z, vw[u].w);
-#pragma unroll
-            for (int m = 0; m < RT; ++m)
-#pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[m][p][0], o[m][u], 0, 0, 0);
-                    o[m][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[m][p][1], o[m][u], 0, 0, 0);
-                }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (t + 4 < t1) load_v(t + 4, vid);
-        kid = kid2; vid = vid2;
+                for (int i = 0; i < 4; ++i) squares = __builtin_fmaf(o[m][u][i], o[m][u][i], squares);
+        if (down != 0.f || __builtin_amdgcn_ballot_w64(!(squares < INFINITY)) == 0) break;
     }
 
+    // (where a lane is, counted anew: nothing of it is held over the loop, whose registers are all taken with two row tiles)
+    const int at_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), at_li = at_lane & 15, at_quad = at_lane >> 4;
+    const int at_tid = 64 * wave + at_lane;
     // the wavefronts' parts of a row, brought to the largest reference
     const bool any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
 #pragma unroll
@@ -492,12 +508,12 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
         const float total = any_bad ? __uint_as_float(0x7fc00000u) : quad_sum(sum[m]);
 #pragma unroll
         for (int u = 0; u < DT; ++u)
-            if (16 * u < a.d) *(f32x4*)(joint + (wave * ROWS + 16 * m + li) * pitch + 16 * u + 4 * quad) = o[m][u];
-        if (quad == 0) ml[wave * ROWS + 16 * m + li] = float2{ref[m], total};
+            if (16 * u < a.d) *(f32x4*)(joint + (wave * ROWS + 16 * m + at_li) * pitch + 16 * u + 4 * at_quad) = o[m][u];
+        if (at_quad == 0) ml[wave * ROWS + 16 * m + at_li] = float2{ref[m], total};
     }
     __syncthreads();
     const int n_rows = rows - r_base < ROWS ? rows - r_base : ROWS, dq = a.d / 4;
-    for (int q = tid; q < n_rows * dq; q += 256) {
+    for (int q = at_tid; q < n_rows * dq; q += 256) {
         const int i = q / dq, f = q % dq * 4;
         float m = -INFINITY, total = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -123,14 +123,21 @@ template <typename T, int C> __device__ __forceinline__ int swizzle_v(int row) {
     return C % 16 == 0 ? 4 * (row & 3) : C % 8 == 0 ? 4 * ((row >> 1) & 1) : 0;
 }
 
+// Outputs are accumulated before they are divided by the sum, with weights of up to 2^8, so that finite values of V above 2^120 / keys
+// may pass the largest float where their mean does not.  Whoever finds outputs at the end whose squares do not add up to a float
+// (one of 2^64 or more, or not finite) goes over the keys once more with weights that are smaller by `headroom` powers of two: then
+// all together come to half the largest |v| at most, and weights that this makes 0 are below 2^-87 of the row's largest.
+__device__ __forceinline__ float headroom(int keys) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)(41 - __builtin_clz(keys | 1))))); }
+
 // What a wavefront accumulates for 32 rows, and what becomes of a tile's scores.
 template <int DT>
 struct PromptAcc {
     f32x16 o[DT];
     float ref, off, sum;                  // reference score, what a weight's exponent takes off for it, this lane's share of the row's sum
+    float down;                           // powers of two that all weights are smaller by (see headroom)
     int lim;                              // keys that the lane's row sees
-    __device__ __forceinline__ void clear() {
-        ref = -INFINITY; off = 0.f; sum = 0.f;
+    __device__ __forceinline__ void clear(float smaller) {
+        ref = -INFINITY; off = 0.f; sum = 0.f; down = smaller;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -154,7 +161,7 @@ struct PromptAcc {
         mx = pair_max(mx);
         if (__builtin_amdgcn_ballot_w64((mx - ref) * sl > 8.f) != 0) {      // (both lanes of a pair agree; -inf against -inf is no)
             // before a row's first score there is nothing to rescale, and no offset that means anything
-            const float nm = fmaxf(mx, ref), to = nm == -INFINITY ? 0.f : -nm * sl;
+            const float nm = fmaxf(mx, ref), to = nm == -INFINITY ? 0.f : -nm * sl - down;
             const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(to - off);
             ref = nm;
             off = to;
@@ -183,9 +190,9 @@ struct PromptRows : PromptAcc<DT> {
     uint4 qf[NK];
 
     // row r of key head hk's rows
-    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, int lane) {
+    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, float down, int lane) {
         const int lh = lane >> 5, dc = a.d / EPC;
-        this->clear();
+        this->clear(down);
         this->lim = limit;
         const int token = a.G.token(r);
         const T* q = (const T*)a.Q + (long long)(first + token) * a.q_token + (long long)(hk * a.G.size + r - token * a.G.size) * a.q_head;
@@ -281,9 +288,9 @@ struct PromptRowsParts : PromptAcc<DT> {
         mfma_group<bf16_t>(x[1], y[0], acc);
         mfma_group<bf16_t>(x[0], y[0], acc);
     }
-    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, int lane) {
+    __device__ __forceinline__ void init(const PromptArgs& a, int first, int hk, int r, int limit, float down, int lane) {
         const int lh = lane >> 5;
-        this->clear();
+        this->clear(down);
         this->lim = limit;
         const int token = a.G.token(r);
         const float* q = (const float*)a.Q + (long long)(first + token) * a.q_token + (long long)(hk * a.G.size + r - token * a.G.size) * a.q_head;
@@ -344,14 +351,23 @@ struct PromptRowsParts : PromptAcc<DT> {
     }
 };
 template <int DT>
-__device__ __forceinline__ bool suspect(const PromptAcc<DT>& a) {
+__device__ __forceinline__ bool has_large(const PromptAcc<DT>& a) {
+    float squares[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) squares[v & 7] = __builtin_fmaf(a.o[dt][v], a.o[dt][v], squares[v & 7]);
+    return !((squares[0] + squares[1]) + (squares[2] + squares[3]) + ((squares[4] + squares[5]) + (squares[6] + squares[7])) < INFINITY);
+}
+template <int DT>
+__device__ __forceinline__ SplitSuspect magnitudes(const PromptAcc<DT>& a) {
     SplitSuspect t;
     t.add(a.sum);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int v = 0; v < 16; ++v) t.add(a.o[dt][v]);
-    return t.any();
+    return t;
 }
 
 // A sequence's keys in steps of KEYS: a step's pieces go from memory straight into LDS, piece q of the tile at its place there;
@@ -441,7 +457,8 @@ struct PromptPlace {
         b = pair / a.Hkv;
         hk = pair - b * a.Hkv;
         const PackedSpan qs(a.q_off, b, a.n_q), ks(a.k_off, b, a.n_k);
-        q_first = qs.first; q_count = qs.count; k_first = ks.first; nk = ks.count;
+        q_first = __builtin_amdgcn_readfirstlane(qs.first); q_count = __builtin_amdgcn_readfirstlane(qs.count);
+        k_first = __builtin_amdgcn_readfirstlane(ks.first); nk = __builtin_amdgcn_readfirstlane(ks.count);
         rows = (q_count < a.max_q ? q_count : a.max_q) * G.size;
         r_base = (a.tiles - 1 - (int)blockIdx.y) * ROWS;
         r_end = r_base + ROWS < rows ? r_base + ROWS : rows;
@@ -466,6 +483,22 @@ struct PromptPlace {
     }
 };
 
+// The second pass for large outputs (headroom), next to never taken, starts from the kernel's arguments as they lie in memory, so that the
+// first holds no registers for it (where it did, 96 heads x 274 rows, d 64, took 11.9 us and 32 x 300 11.0; 11.4 and 10.1 so; 11.2 and
+// 9.9 without a second pass).
+__device__ __forceinline__ void arguments_anew(PromptArgs* to) {
+    typedef const uint64_t __attribute__((address_space(4)))* kernarg;
+    kernarg from = (kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(from));
+    union Words { PromptArgs a; uint64_t w[sizeof(PromptArgs) / 8]; __device__ Words() {} } u;
+    static_assert(sizeof(PromptArgs) % 8 == 0, "whole words");
+#pragma unroll
+    for (size_t i = 0; i < sizeof(PromptArgs) / 8; ++i) u.w[i] = from[i];
+    *to = u.a;
+    auto global = [](auto& p) { p = (std::remove_reference_t<decltype(p)>)(const __attribute__((address_space(1))) char*)p; };      // (what a kernel's argument is known to be)
+    global(to->Q); global(to->K); global(to->V); global(to->O); global(to->lse); global(to->q_off); global(to->k_off); global(to->part);
+}
+
 // Long sequences, bf16: four wavefronts of 32 rows each go over the same keys, 64 at a time, which they stage together, the next step's
 // while one is worked on.  Two wavefronts per SIMD fill each other's waits between products (32 a step), exponentials (32 at a
 // quarter of the rate) and fragment reads (32 KB a step, at 128 bytes a cycle and CU just below the products' time).
@@ -473,8 +506,9 @@ struct PromptPlace {
 // product of two 16384 x 16384 matrices reaches 1400; matrix units busy a third of the cycles, vector instructions 40 %, no bank
 // conflicts.  With the tiles in staging registers (244 instead of 206) 1.35 ms; with the odd values' products in the loop (410
 // registers, one wavefront per SIMD) 2.14.
+// One pass over the keys; true: outputs are too large for it (see headroom), and `again` has to be.
 template <int DT>
-__global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+__device__ __forceinline__ bool prompt_pass(const PromptArgs& a, int tid, bool again) {
     typedef bf16_t T;
     typedef PromptRows<T, DT, 2> Rows;
     constexpr int C = Rows::C, D = Rows::D, KEYS = 64, THREADS = 64 * kPromptWaves;
@@ -483,10 +517,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     OddColumn* const oddc = (OddColumn*)(lds + 4 * KEYS * C);
     int* const any_odd = (int*)(oddc + D);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr_t)lds;
-    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const PromptPlace<32 * kPromptWaves> at(a);
-    if (at.r_base >= at.rows) return;
+    if (at.r_base >= at.rows) return false;
     const int w_base = at.r_base + wave * 32;
     const bool active = w_base < at.rows;
     const int w_end = w_base + 32 < at.rows ? w_base + 32 : at.rows;
@@ -494,14 +528,17 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     int t0, t1;
     at.steps<KEYS>(a.shares, &t0, &t1);
     const Keys keys(a, at.k_first, at.nk, at.hk, tid);
-    if (t0 < t1) keys.load_both(t0, lds0 + (t0 & 1) * 2 * Keys::TILE, wave, tid);
-    if (keys.dc < C) keys.clear(lds, 4, tid);
-    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
-    if (tid == 0) *any_odd = 0;
+    int* const any_large = any_odd + 1;
     Rows rows;
     const bool ok = w_base + li < at.rows;
     const int r = ok ? w_base + li : at.rows - 1;
-    rows.init(a, at.q_first, at.hk, r, at.limit(r), lane);
+    if (t0 < t1) keys.load_both(t0, lds0 + (t0 & 1) * 2 * Keys::TILE, wave, tid);
+    if (!again) {
+        if (keys.dc < C) keys.clear(lds, 4, tid);
+        for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
+        if (tid == 0) *any_odd = *any_large = 0;
+    }
+    rows.init(a, at.q_first, at.hk, r, at.limit(r), again ? headroom(at.nk) : 0.f, lane);
     for (int t = t0; t < t1; ++t) {
         const uint32_t sk = lds0 + (t & 1) * 2 * Keys::TILE;
         wait_staged();
@@ -514,8 +551,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
         if (t * KEYS >= w_hi) continue;              // (uniform over the wavefront: none of its rows sees these keys)
         rows.step(sk, sk + Keys::TILE, t * KEYS, (t + 1) * KEYS > w_lo, a.sl, lane, [] {}, [] {});
     }
+    if (!again && has_large(rows)) *any_large = 1;   // (set up before the first step's barrier)
     __syncthreads();                                 // (the last steps' odd values are noted)
-    if (!active) return;
+    if (!again && __builtin_expect(*any_large, 0)) return true;
+    if (!active) return false;
 
     const float total = pair_sum(rows.sum);
     const int token = a.G.token(r), head = at.hk * a.G.size + r - token * a.G.size;
@@ -529,7 +568,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
     }
     if (a.shares > 1) {
         const long long all = (long long)a.n_q * a.Hq, p0 = (long long)at.share * all + row * a.Hq + head;
-        if (!ok) return;
+        if (!ok) return false;
         float* p = a.part + p0 * a.d;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -539,7 +578,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
                 if (col < a.d) *(float4*)(p + col) = float4{o[dt][4 * g], o[dt][4 * g + 1], o[dt][4 * g + 2], o[dt][4 * g + 3]};
             }
         if (lh == 0) ((float2*)(a.part + (long long)a.shares * all * a.d))[p0] = float2{total == 0.f ? INFINITY : rows.off, total};
-        return;
+        return false;
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;      // (a row that saw nothing is 0)
     if (a.lse && ok && lh == 0) a.lse[(long long)head * a.n_q + row] = total == 0.f ? -INFINITY : 0.69314718055994531f * (__log2f(total) - rows.off);
@@ -559,6 +598,16 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
             if (ok && col < a.d) *(uint4*)(out + col) = uint4{s0[0], s1[0], s0[1], s1[1]};
         }
     }
+    return false;
+}
+template <int DT>
+__global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_kernel(PromptArgs a) {
+    if (__builtin_expect(!prompt_pass<DT>(a, threadIdx.x, false), 1)) return;
+    PromptArgs anew;
+    arguments_anew(&anew);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    prompt_pass<DT>(anew, tid, true);
 }
 
 // Few rows, and float tensors of any length: a workgroup has 32 rows, and its wavefronts divide the keys, every W-th 32 of them
@@ -578,7 +627,7 @@ template <typename T, int DT> constexpr int prompt_split_lds() {
     return prompt_split_waves<T, DT>() * (prompt_split_tile<T, DT>() + 32 * 8) + 32 * DT * 12 + 16;
 }
 template <typename T, int DT>
-__global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_split_kernel(PromptArgs a) {
+__device__ __forceinline__ bool prompt_split_pass(const PromptArgs& a, int tid, bool again) {      // (as prompt_pass)
     typedef PromptRows<T, DT, 1> Rows;
     constexpr int C = Rows::C, D = Rows::D, KEYS = 32, W = prompt_split_waves<T, DT>(), THREADS = 64 * W;
     typedef PromptKeys<T, C, KEYS, 64> Keys;
@@ -586,26 +635,29 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
     extern __shared__ uint4 lds[];
     OddColumn* const oddc = (OddColumn*)(lds + W * 2 * KEYS * C);
     int* const any_odd = (int*)(oddc + D);
+    int* const any_large = any_odd + 1;
     float2* const ml = (float2*)(any_odd + 4);
-    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const PromptPlace<32> at(a);
-    if (at.r_base >= at.rows) return;
+    if (at.r_base >= at.rows) return false;
     int t0, t1;
     at.steps<KEYS>(a.shares, &t0, &t1);
     const Keys keys(a, at.k_first, at.nk, at.hk, lane);
     uint4* const own = lds + wave * 2 * KEYS * C;
     const uint32_t sk = (uint32_t)(uintptr_t)(lds_ptr_t)own;
-    if (keys.dc < C) keys.clear(own, 2, lane);
-    for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
-    if (tid == 0) *any_odd = 0;
+    if (!again) {
+        if (keys.dc < C) keys.clear(own, 2, lane);
+        for (int i = tid; i < D; i += THREADS) oddc[i] = OddColumn{kNoKey, kNoKey, kNoKey};
+        if (tid == 0) *any_odd = *any_large = 0;
+    }
     const int lane_row = at.r_base + li < at.rows ? at.r_base + li : at.rows - 1, lane_limit = at.limit(lane_row);
     PromptAcc<DT> acc;
-    auto go = [&](auto rows) {
+    auto go = [&](auto rows, float down) {
         // K's tile is asked for again as soon as it has been read, V's too: each has the other's work to arrive in.  (A wavefront
         // has 64 lanes' part in every request, so PIECES requests are one tile.)
         if (t0 + wave < t1) keys.load_both(t0 + wave, sk, 0, lane);
-        rows.init(a, at.q_first, at.hk, lane_row, lane_limit, lane);
+        rows.init(a, at.q_first, at.hk, lane_row, lane_limit, down, lane);
         __syncthreads();                             // (the columns' odd values are set up)
         for (int t = t0 + wave; t < t1; t += W) {
             const bool masked = (t + 1) * KEYS > at.lo, more = t + W < t1;
@@ -626,15 +678,19 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
         acc = rows;
     };
     if constexpr (Rows::BF || DT > 4) {              // (256 features in three parts do not fit the registers)
-        go(Rows{});
+        go(Rows{}, again ? headroom(at.nk) : 0.f);
+        if (!again && has_large(acc)) *any_large = 1;
     } else {
-        go(PromptRowsParts<DT>{});
-        if (__syncthreads_or(suspect(acc))) go(Rows{});
+        go(PromptRowsParts<DT>{}, 0.f);
+        const SplitSuspect seen = magnitudes(acc);
+        const bool large = seen.high >= 2 * __float_as_uint(0x1p64f);
+        if (__syncthreads_or(large || seen.any())) go(Rows{}, __syncthreads_or(large) ? headroom(at.nk) : 0.f);
     }
     // the wavefronts' parts of a row, brought to the smallest offset
     const float sum = pair_sum(acc.sum);
     if (lh == 0) ml[wave * 32 + li] = float2{sum == 0.f ? INFINITY : acc.off, sum};
     __syncthreads();                                 // (staging is free, odd values are noted)
+    if (!again && __builtin_expect(*any_large, 0)) return true;
     float* const joint = (float*)lds;
     {
         float off = INFINITY;
@@ -682,6 +738,18 @@ __global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_spl
         T* out = (T*)a.O + row * a.o_token + (long long)head * a.o_head + c;
         if constexpr (Rows::BF) *(uint2*)out = uint2{f2bf_pk(x[0] * inv, x[1] * inv), f2bf_pk(x[2] * inv, x[3] * inv)};
         else *(float4*)out = float4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    }
+    return false;
+}
+template <typename T, int DT>
+__global__ __launch_bounds__((64 * prompt_split_waves<T, DT>())) void prompt_split_kernel(PromptArgs a) {
+    if (__builtin_expect(!prompt_split_pass<T, DT>(a, threadIdx.x, false), 1)) return;
+    if constexpr (sizeof(T) == 2 || DT > 4) {        // (the others have been over their keys once more themselves)
+        PromptArgs anew;
+        arguments_anew(&anew);
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        prompt_split_pass<T, DT>(anew, tid, true);
     }
 }
 

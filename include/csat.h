@@ -267,7 +267,8 @@ typedef struct {
  * (an empty sequence, causal with fewer keys than rows), or only scores of -inf, is 0 with lse = -inf.  What a masked
  * or foreign row of K or V holds, an infinity or NaN included, has no effect.  bf16: the weights are rounded to bf16 (by at
  * most 2^-8 of each) for the product with V, everything else is float.  Values of V of up to 2^127 give outputs that are as right as others
- * (attention over the cache too); scores are float, one beyond its range is infinite.
+ * (attention over the cache too); scores are float, one beyond its range is infinite.  float: with up to 128 features a value of Q or K below
+ * 2^-109 counts as the nearest multiple of 2^-133 (over the cache: one of Q, with any), and so does a weight, next to the row's largest.
  * Workspace: csat_prompt_workspace_bytes (host-only query; it may be 0, workspace may then be NULL). */
 csat_status csat_prompt_workspace_bytes(const csat_packed_dims* dims, size_t* bytes);
 csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const void* Q, const void* K, const void* V,

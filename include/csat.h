@@ -252,7 +252,8 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
  * bound are not written, the others keep the places that they have among all of the sequence's rows.  (csat_prompt_attention: rows see
  * all keys whatever max_k says, which only shapes the work.)  Rows of no sequence (behind the last offset) are left as they were.
  * d: a multiple of 8 (csat_prompt_attention) or of 16 (the cache), at most 256.  n_q, n_k, max_q, max_k at least 1; B at most
- * 65535, n_q * Hq, n_k and a cache's max_pages * page at most 2^30.
+ * 65535, B * Hq at most 2^22 - 1, n_q * Hq, n_k and a cache's max_pages * page at most 2^30, Hkv times the pages that max_len takes at
+ * most 2^21 - 1.
  * ------------------------------------------------------------------------------------------------------ */
 typedef struct {
     int B, Hq, Hkv, d;
@@ -320,7 +321,8 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
  * the smallest scale for what they hold; W_to [B, Hkv, to->max_pages * page] gets their weights,
  * kept [B, Hkv, budget] int32 their slots in `from` (-1 behind them), to->lengths their number.  Every head keeps tokens of its own.
  * to->max_len and to->max_pages * page must be at least min(budget, from->max_len), else CSAT_ERR_SHAPE; W_to, to->table and
- * to->lengths must be others than W, from->table and from->lengths (other heads still read those), else CSAT_ERR_PARAM. */
+ * to->lengths must be others than W, from->table and from->lengths (other heads still read those), else CSAT_ERR_PARAM.  B * Hkv * budget at
+ * most 2^30. */
 csat_status csat_cache_evict(void* ctx, const csat_packed_dims* dims, const csat_cache* from, const csat_cache* to,
                              const float* W, float* W_to, int budget, int recent, int* kept, void* stream);
 

@@ -2244,7 +2244,8 @@ CacheView cache_view(const csat_cache& c) {
     return v;
 }
 
-struct CachedPlan { int row_tiles, tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; };
+struct CachedPlan { int row_tiles, tiles, shares, share_tokens, score_ld; size_t part_bytes, bytes; bool fits; };
+constexpr size_t kMostScoreBytes = (size_t)1 << 60;
 // Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike: 512, more where a
 // sequence would have more shares than it takes to occupy the chip twice (one sequence of 131072 tokens, 8 key heads: 58 us with
 // shares of 2048, 63, 72, 92 with 1024, 512, 256, whose join grows; 32 sequences of 700 to 8100: 92 us with 512, 100 with 2048).
@@ -2255,10 +2256,12 @@ CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weig
     p.tiles = (int)((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
     const long long groups = (long long)d.B * d.Hkv * p.tiles, most = std::max({512 / groups, std::min(64LL, 8192 / groups), 16LL});
     p.share_tokens = (int)std::max(512LL, round_up((c.max_len + most - 1) / most, 256));
-    p.shares = (c.max_len + p.share_tokens - 1) / p.share_tokens;
+    p.shares = (c.max_len + p.share_tokens - 1) / p.share_tokens;      // (at most 512)
     p.score_ld = (int)round_up(c.max_len, 64);
     p.part_bytes = p.shares > 1 || weights ? (size_t)round_up((long long)p.shares * d.n_q * d.Hq * (d.d + 2) * 4, 256) : 0;
-    p.bytes = p.part_bytes + (weights ? (size_t)d.B * d.Hkv * rows * p.score_ld * 4 : 0);
+    const unsigned __int128 scores = weights ? (unsigned __int128)rows * d.B * d.Hkv * p.score_ld * 4 : 0;
+    p.fits = scores <= kMostScoreBytes;
+    p.bytes = p.fits ? p.part_bytes + (size_t)scores : 0;
     return p;
 }
 
@@ -2846,7 +2849,6 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_offsets) || !aligned16(k_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace))
         return CSAT_ERR_ALIGN;
     const PromptPlan p = prompt_plan(d);
-    if (p.tiles > kMaxBlocksYZ || (p.shares > 1 && (long long)d.B * longest_q(d) * d.Hq > kMaxBlocks)) return CSAT_ERR_SHAPE;
     if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
     OptionScope scope(ctx);
     hipStream_t st = (hipStream_t)stream;
@@ -2899,16 +2901,18 @@ csat_status csat_cache_workspace_bytes(const csat_packed_dims* dims, const csat_
     CSAT_TRY(check_packed(dims, 16));
     CSAT_TRY(check_cache(*dims, cache));
     if (!bytes) return CSAT_ERR_NULL;
-    *bytes = cached_plan(*dims, *cache, true).bytes;
-    return CSAT_OK;
+    const CachedPlan p = cached_plan(*dims, *cache, true);
+    *bytes = p.bytes;
+    return p.fits ? CSAT_OK : CSAT_ERR_SHAPE;
 }
 
 csat_status csat_cache_workspace_bytes_without_weights(const csat_packed_dims* dims, const csat_cache* cache, size_t* bytes) {
     CSAT_TRY(check_packed(dims, 16));
     CSAT_TRY(check_cache(*dims, cache));
     if (!bytes) return CSAT_ERR_NULL;
-    *bytes = cached_plan(*dims, *cache, false).bytes;
-    return CSAT_OK;
+    const CachedPlan p = cached_plan(*dims, *cache, false);
+    *bytes = p.bytes;
+    return p.fits ? CSAT_OK : CSAT_ERR_SHAPE;
 }
 
 csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const csat_cache* cache, const void* Q,
@@ -2925,8 +2929,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(q_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(W) || !aligned16(workspace)) return CSAT_ERR_ALIGN;
     const CachedPlan p = cached_plan(d, *cache, W != nullptr);
-    if ((long long)d.Hkv * p.tiles > kMaxBlocks || p.shares > kMaxBlocksYZ ||
-        (long long)d.B * longest_q(d) * d.Hq + (long long)d.B * d.Hkv * ((cache->max_len + 1023) / 1024) > kMaxBlocks) return CSAT_ERR_SHAPE;
+    if (!p.fits) return CSAT_ERR_SHAPE;
     if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return CSAT_ERR_WORKSPACE;
     OptionScope scope(ctx);
     hipStream_t st = (hipStream_t)stream;

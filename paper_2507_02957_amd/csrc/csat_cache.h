@@ -226,6 +226,7 @@ struct CachedArgs {
     Group G;
     float sl;                      // scale log2(e)
     int tiles, row_tiles;          // workgroups per sequence, key head and share, 16-row tiles in each
+    int first_tile;                // of this launch
     int shares, share_tokens;      // the longest sequence's shares of share_tokens (a multiple of 64); a sequence has those it needs
     float* part;                   // [shares][n_q Hq][d], then [shares][n_q Hq][2] as in csat_prompt.h, or null: O and lse are written
     float* scores;                 // [B][Hkv][max_q G.size][score_ld] in units of log2, for the weights, or null
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = blockIdx.z, share = blockIdx.y, tile = a.tiles == 1 ? 0 : blockIdx.x / a.Hkv, hk = blockIdx.x - tile * a.Hkv;
     const PackedSpan qs(a.q_off, b, a.n_q);
-    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size, r_base = ROWS * tile;
+    const int rows = (qs.count < a.max_q ? qs.count : a.max_q) * a.G.size, r_base = ROWS * (a.first_tile + tile);
     if (r_base >= rows) return;
     int L = a.c.lengths[b];
     bool bad = L < 0 || L > a.c.max_len;
@@ -546,20 +547,20 @@ __global__ __launch_bounds__(256, DC <= 2 ? 2 : 1) void cache_attention_kernel(C
     }
 }
 
-// The second launch: the first o_blocks workgroups join the rows of O, the others form W = decay W + sum over rows of
-// 2^(score - lse) for 1024 tokens of a sequence and key head, a thread four of them.
+// The second launch, y a sequence: its first o_blocks workgroups join the rows of O, the others form W = decay W + sum over rows of
+// 2^(score - lse) for 1024 tokens of a key head, a thread four of them.  first_block: of this launch.
 template <typename T>
-__global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs a, int o_blocks) {
+__global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs j, CachedArgs a, int o_blocks, int first_block) {
     constexpr int RB = 64;
     __shared__ float lse2[RB];
     __shared__ int limit[RB];
-    if ((int)blockIdx.x < o_blocks) {
-        join_block<T>(j, blockIdx.x);
+    const int b = blockIdx.y, block = first_block + blockIdx.x;
+    if (block < o_blocks) {
+        join_block<T>(j, b, block);
         return;
     }
     const int tid = threadIdx.x, lane = tid & 63;
-    const int chunks = (a.c.max_len + 1023) / 1024, id = blockIdx.x - o_blocks;
-    const int chunk = id % chunks, hk = id / chunks % a.Hkv, b = id / chunks / a.Hkv;
+    const int chunks = (a.c.max_len + 1023) / 1024, id = block - o_blocks, hk = id / chunks, chunk = id - hk * chunks;
     const int L = a.c.lengths[b], t = chunk * 1024 + 4 * tid;
     if (L < 0 || L > a.c.max_len || chunk * 1024 >= L) return;
     const PackedSpan qs(a.q_off, b, a.n_q);

@@ -38,7 +38,7 @@ struct PromptArgs {
     int B, Hq, Hkv, d, n_q, n_k, max_q, causal;
     Group G;
     float sl;                      // scale log2(e)
-    int tiles;                     // row tiles per sequence and key head
+    int tiles;                     // row tiles per sequence and key head, up to the end of this launch's
     int pair_groups;               // (sequence, key head) pairs / the grid's x
     int shares;                    // > 1: workgroups that split a row tile's keys, joined by attention_join_kernel
     float* part;                   // [shares][n_q Hq][d] unnormalised outputs, then [shares][n_q Hq][2]: offset, sum
@@ -873,15 +873,14 @@ __device__ __forceinline__ void join_row_few(const JoinArgs& a, int b, int r) {
     if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{f2bf_pk(o.x * inv, o.y * inv), f2bf_pk(o.z * inv, o.w * inv)};
     else *(float4*)out = float4{o.x * inv, o.y * inv, o.z * inv, o.w * inv};
 }
-// the workgroups that all rows need, and which a workgroup has
+// the workgroups that a sequence's rows need, and which a workgroup has
 __host__ __device__ inline int join_blocks_per_sequence(int max_q, int Hq, int shares) { return shares <= kJoinFew ? (max_q * Hq + 3) / 4 : max_q * Hq; }
 template <typename T>
-__device__ __forceinline__ void join_block(const JoinArgs& a, int block) {
-    const int per = join_blocks_per_sequence(a.max_q, a.Hq, a.shares), b = block / per, r = block % per;
-    if (a.shares <= kJoinFew) join_row_few<T>(a, b, 4 * r + (threadIdx.x >> 6));
-    else join_row<T>(a, b, r);
+__device__ __forceinline__ void join_block(const JoinArgs& a, int b, int block) {
+    if (a.shares <= kJoinFew) join_row_few<T>(a, b, 4 * block + (threadIdx.x >> 6));
+    else join_row<T>(a, b, block);
 }
 template <typename T>
-__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) { join_block<T>(a, blockIdx.x); }
+__global__ __launch_bounds__(256) void attention_join_kernel(JoinArgs a) { join_block<T>(a, blockIdx.y, blockIdx.x); }
 
 }  // namespace csat

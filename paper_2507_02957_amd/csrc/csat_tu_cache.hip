@@ -22,21 +22,33 @@ hipError_t cache_store_launch(bool bf16, const StoreArgs& a, hipStream_t st) {
 #undef CSAT_STORE
 }
 
-hipError_t cache_attention_launch(bool bf16, const CachedArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.Hkv * a.tiles), (unsigned)a.shares, (unsigned)a.B);
+constexpr int kMostBlocks = (1 << 22) - 1;      // of the grid's x; what needs more takes several launches
+
+hipError_t cache_attention_launch(bool bf16, const CachedArgs& all, hipStream_t st) {
+    CachedArgs a = all;
+    const int most = kMostBlocks / a.Hkv;
+    for (int n; a.first_tile < a.tiles; a.first_tile += n) {
+        n = a.tiles - a.first_tile < most ? a.tiles - a.first_tile : most;
+        const dim3 grid((unsigned)(a.Hkv * n), (unsigned)a.shares, (unsigned)a.B);
 #define CSAT_CACHED(T_, DC_, RT_) launch(cache_attention_kernel<T_, DC_, RT_>, grid, 256, cached_lds_bytes<DC_, RT_>(a.d), st, a)
-    if (!bf16) return a.d <= 64 ? CSAT_CACHED(float, 1, 1) : a.d <= 128 ? CSAT_CACHED(float, 2, 1) : CSAT_CACHED(float, 4, 1);
-    if (a.row_tiles == 2) return a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 2) : CSAT_CACHED(bf16_t, 2, 2);
-    return a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 1) : a.d <= 128 ? CSAT_CACHED(bf16_t, 2, 1) : CSAT_CACHED(bf16_t, 4, 1);
+        const hipError_t e = !bf16 ? (a.d <= 64 ? CSAT_CACHED(float, 1, 1) : a.d <= 128 ? CSAT_CACHED(float, 2, 1) : CSAT_CACHED(float, 4, 1))
+                             : a.row_tiles == 2 ? (a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 2) : CSAT_CACHED(bf16_t, 2, 2))
+                                                : (a.d <= 64 ? CSAT_CACHED(bf16_t, 1, 1) : a.d <= 128 ? CSAT_CACHED(bf16_t, 2, 1) : CSAT_CACHED(bf16_t, 4, 1));
 #undef CSAT_CACHED
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t cache_join_launch(bool bf16, const JoinArgs& j, const CachedArgs& a, hipStream_t st) {
-    const long long o_blocks = (long long)a.B * join_blocks_per_sequence(a.max_q, a.Hq, a.shares), w_blocks = a.scores ? (long long)a.B * a.Hkv * ((a.c.max_len + 1023) / 1024) : 0;
-    const dim3 grid((unsigned)(o_blocks + w_blocks));
-    if (bf16) hipLaunchKernelGGL(cache_join_kernel<bf16_t>, grid, dim3(256), 0, st, j, a, (int)o_blocks);
-    else hipLaunchKernelGGL(cache_join_kernel<float>, grid, dim3(256), 0, st, j, a, (int)o_blocks);
-    return hipGetLastError();
+    const int o_blocks = join_blocks_per_sequence(a.max_q, a.Hq, a.shares), all = o_blocks + (a.scores ? a.Hkv * ((a.c.max_len + 1023) / 1024) : 0);
+    for (int first = 0, n; first < all; first += n) {
+        n = all - first < kMostBlocks ? all - first : kMostBlocks;
+        const dim3 grid((unsigned)n, (unsigned)a.B);
+        const hipError_t e = bf16 ? launch(cache_join_kernel<bf16_t>, grid, 256, 0, st, j, a, o_blocks, first) : launch(cache_join_kernel<float>, grid, 256, 0, st, j, a, o_blocks, first);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t cache_evict_launch(const EvictArgs& a, int blocks, hipStream_t st) {

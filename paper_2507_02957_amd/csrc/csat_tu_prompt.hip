@@ -22,8 +22,15 @@ hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, bool split, hipStream_
             const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.Hkv / a.pair_groups), (unsigned)a.tiles, (unsigned)(a.shares > 1 ? a.shares : a.pair_groups)), dim3(threads), lds_bytes, st, a);
-        return hipGetLastError();
+        // (the grid's y holds 65535 tiles; the last ones, the longest, first)
+        PromptArgs part = a;
+        for (int n; part.tiles > 0; part.tiles -= n) {
+            n = part.tiles < 65535 ? part.tiles : 65535;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(a.B * a.Hkv / a.pair_groups), (unsigned)n, (unsigned)(a.shares > 1 ? a.shares : a.pair_groups)), dim3(threads), lds_bytes, st, part);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
 #if CSAT_TU_BF16
 #define CSAT_PROMPT(DT_) (split ? launch(prompt_split_kernel<T, DT_>, 64 * prompt_split_waves<T, DT_>(), prompt_split_lds<T, DT_>()) \
@@ -39,7 +46,7 @@ hipError_t CSAT_TU_FN(prompt_launch)(const PromptArgs& a, bool split, hipStream_
 }
 
 hipError_t CSAT_TU_FN(attention_join_launch)(const JoinArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)((long long)a.B * join_blocks_per_sequence(a.max_q, a.Hq, a.shares))), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(attention_join_kernel<T>, dim3((unsigned)join_blocks_per_sequence(a.max_q, a.Hq, a.shares), (unsigned)a.B), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

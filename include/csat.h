@@ -281,7 +281,8 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
  * [pages, Hkv, page, d], V codes [pages, Hkv, d, page] (a token's values a page apart, the order in which the
  * attention's matrix instructions take them).  A sequence's tokens are the first lengths[b] slots of the pages that row b of
  * table (device int32 [B, max_pages]) names; entries beyond them are not read.  max_len bounds lengths[b] (it sizes
- * the grids; at most max_pages * page).  Pages may be shared by sequences as long as they are only read.
+ * the grids; at most max_pages * page).  Pages may be shared by sequences as long as they are only read.  Hkv and d of a call's dims are the
+ * pool's, which the structure does not hold: no call from C can check them.
  * Errors in what only the device sees: a sequence whose length is negative or above max_len (to store: or below the new
  * rows), or one of whose needed table entries names no page of the pool, gives NaN in its rows of O and lse (its weights are then
  * undefined), is not stored to, and is evicted to length -1 with nothing but kept = -1 written for it; memory outside the given

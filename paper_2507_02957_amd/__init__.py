@@ -167,15 +167,21 @@ def make_packed_dims(B, Hq, Hkv, d, n_q, n_k, max_q, max_k, dtype, causal=True, 
 def make_cache(K, V, Ks, Vs, table, lengths, max_len=None) -> csat_cache:
     """K: codes [pages, Hkv, page, d], V: [pages, Hkv, d, page] (one byte each, e.g. torch.float8_e4m3fn), Ks, Vs: float32
     [pages, Hkv], table: int32 [B, max_pages], lengths: int32 [B], all contiguous; max_len: the longest length (default: what the
-    table has room for).  The structure holds the tensors' addresses and keeps them alive."""
-    pages, _, page, _ = K.shape
-    for t in (K, V, Ks, Vs, table, lengths):
+    table has room for).  The structure holds the tensors' addresses and keeps them alive; calls whose dims are not those of its tensors
+    are refused."""
+    import torch
+    pages, heads, page, d = K.shape
+    B, max_pages = table.shape
+    for t, shape, size in ((K, (pages, heads, page, d), 1), (V, (pages, heads, d, page), 1), (Ks, (pages, heads), torch.float32), (Vs, (pages, heads), torch.float32),
+                           (table, (B, max_pages), torch.int32), (lengths, (B,), torch.int32)):
         if not t.is_contiguous():
             raise ValueError("the tensors of a cache are contiguous")
-    max_pages = table.shape[1]
+        if tuple(t.shape) != shape or (t.element_size() if size == 1 else t.dtype) != size:
+            raise ValueError(f"a tensor of the cache is {t.dtype} {tuple(t.shape)}, not {'of one byte' if size == 1 else size} {shape}")
     c = csat_cache(pages, page, max_pages, max_pages * page if max_len is None else max_len, K.data_ptr(), V.data_ptr(), Ks.data_ptr(),
                    Vs.data_ptr(), table.data_ptr(), lengths.data_ptr())
     c.tensors = (K, V, Ks, Vs, table, lengths)
+    c.shape = (heads, d, B)
     return c
 
 
@@ -390,6 +396,25 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _of_cache(dims, cache):
+    """Dims that are not those of the cache's tensors would address memory outside them (a structure filled in by hand does not say)."""
+    heads, d, B = getattr(cache, "shape", _ANY)
+    if heads and (dims.Hkv != heads or dims.d != d or dims.B > B):
+        raise ValueError(f"dims of {dims.B} sequences, {dims.Hkv} key heads, {dims.d} features for a cache of {B}, {heads}, {d}")
+
+
+_ANY = (0, 0, 0)
+
+
+def _are(name, *tensors):
+    """Offsets and slots are int32, weights and sums float32: a tensor of another type would be read as, or written over by, numbers of that size."""
+    import torch
+    dtype = getattr(torch, name)
+    for t in tensors:
+        if t is not None and t.dtype is not dtype:
+            raise ValueError(f"a tensor of {name} is needed, not {t.dtype}")
+
+
 def csat_prompt_workspace_bytes(dims: csat_packed_dims) -> int:
     out = ctypes.c_size_t()
     _check(load_library().csat_prompt_workspace_bytes(ctypes.byref(dims), ctypes.byref(out)))
@@ -398,12 +423,16 @@ def csat_prompt_workspace_bytes(dims: csat_packed_dims) -> int:
 
 def csat_prompt_attention(dims, Q, K, V, q_offsets, k_offsets, scale, O, lse, workspace, stream=None):
     """q_offsets, k_offsets: int32 device tensors [B + 1]; lse: float32 [Hq, n_q] or None; workspace may be None where none is needed."""
+    _are("int32", q_offsets, k_offsets)
+    _are("float32", lse)
     _issue("csat_prompt_attention", Q, stream, (
         ctypes.byref(dims), Q.data_ptr(), K.data_ptr(), V.data_ptr(), q_offsets.data_ptr(), k_offsets.data_ptr(), scale, O.data_ptr(), _at(lse),
         _at(workspace), 0 if workspace is None else workspace.numel()))
 
 
 def csat_cache_store(dims, cache, K, V, k_offsets, stream=None):
+    _of_cache(dims, cache)
+    _are("int32", k_offsets)
     _issue("csat_cache_store", K, stream, (ctypes.byref(dims), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), k_offsets.data_ptr()))
 
 
@@ -422,6 +451,9 @@ def csat_cache_workspace_bytes_without_weights(dims: csat_packed_dims, cache: cs
 
 def csat_cache_attention(dims, cache, Q, q_offsets, scale, decay, O, lse, W, workspace, stream=None):
     """lse: float32 [Hq, n_q] or None; W: float32 [B, Hkv, max_pages * page] or None."""
+    _of_cache(dims, cache)
+    _are("int32", q_offsets)
+    _are("float32", lse, W)
     _issue("csat_cache_attention", Q, stream, (
         ctypes.byref(dims), ctypes.byref(cache), Q.data_ptr(), q_offsets.data_ptr(), scale, decay, O.data_ptr(), _at(lse), _at(W),
         _at(workspace), 0 if workspace is None else workspace.numel()))
@@ -429,6 +461,10 @@ def csat_cache_attention(dims, cache, Q, q_offsets, scale, decay, O, lse, W, wor
 
 def csat_cache_evict(dims, cache, to, W, W_to, budget, recent, kept, stream=None):
     """kept: int32 [B, Hkv, budget]; to.lengths is written."""
+    _of_cache(dims, cache)
+    _of_cache(dims, to)
+    _are("int32", kept)
+    _are("float32", W, W_to)
     _issue("csat_cache_evict", W, stream, (
         ctypes.byref(dims), ctypes.byref(cache), ctypes.byref(to), W.data_ptr(), W_to.data_ptr(), budget, recent, kept.data_ptr()))
 

@@ -264,7 +264,7 @@ typedef struct {
 } csat_packed_dims;
 
 /* O = softmax(scale Q K^T) V per sequence and head, by one pass over the keys with a running maximum and sum.
- * scale > 0.  lse (float [Hq, n_q], optional): the logarithm of each row's sum of exp(scale q.k).  A row that sees no key
+ * 0 < scale <= 2^127.  lse (float [Hq, n_q], optional): the logarithm of each row's sum of exp(scale q.k).  A row that sees no key
  * (an empty sequence, causal with fewer keys than rows), or only scores of -inf, is 0 with lse = -inf.  What a masked
  * or foreign row of K or V holds, an infinity or NaN included, has no effect.  bf16: the weights are rounded to bf16 (by at
  * most 2^-8 of each) for the product with V, everything else is float.  Values of V of up to 2^127 give outputs that are as right as others

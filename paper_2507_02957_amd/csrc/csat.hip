@@ -2845,7 +2845,7 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
     if (!Q || !K || !V || !q_offsets || !k_offsets || !O) return CSAT_ERR_NULL;
     if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.k_token, d.k_head, e) || !stride_ok(d.v_token, d.v_head, e) || !stride_ok(d.o_token, d.o_head, e) || !output_strides_ok(d))
         return CSAT_ERR_SHAPE;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return CSAT_ERR_PARAM;
+    if (!(scale > 0.f && scale <= 0x1p127f)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(q_offsets) || !aligned16(k_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(workspace))
         return CSAT_ERR_ALIGN;
     const PromptPlan p = prompt_plan(d);
@@ -2926,7 +2926,7 @@ csat_status csat_cache_attention(void* ctx, const csat_packed_dims* dims, const 
     if (!Q || !q_offsets || !O) return CSAT_ERR_NULL;
     const size_t e = esize(d.dtype);
     if (!stride_ok(d.q_token, d.q_head, e) || !stride_ok(d.o_token, d.o_head, e) || !output_strides_ok(d)) return CSAT_ERR_SHAPE;
-    if (!(scale > 0.f) || !std::isfinite(scale) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
+    if (!(scale > 0.f && scale <= 0x1p127f) || !(decay >= 0.f && decay <= 1.f)) return CSAT_ERR_PARAM;
     if (!aligned16(Q) || !aligned16(q_offsets) || !aligned16(O) || !aligned16(lse) || !aligned16(W) || !aligned16(workspace)) return CSAT_ERR_ALIGN;
     const CachedPlan p = cached_plan(d, *cache, W != nullptr);
     if (!p.fits) return CSAT_ERR_SHAPE;

@@ -42,3 +42,12 @@ def test_stated_limits(lib):  # noqa: F811
             assert _query(lib, "csat_prompt_workspace_bytes", d)[0] == code and (not code or _prompt(lib, d) == code)
     d = _dims(B=1024, Hq=4, Hkv=4)
     assert _evict(lib, d, _cache(), _to(), budget=(1 << 18) + 1) == -2              # (1024 x 4 x 2^18 = 2^30 is the most)
+
+
+def test_scales_that_are_no_float_in_units_of_log2_are_refused(lib):  # noqa: F811
+    """Scores are formed as scale log2(e) q.k: above 2^127 that factor is infinite, and 0 times it no number."""
+    d, c = _dims(), _cache()
+    for scale in (1.8e38, 2.4e38, 3.4e38):
+        assert _prompt(lib, d, scale=scale) == -6 and _attend(lib, d, c, scale=scale) == -6
+    few = _dims(n_q=1, max_q=1, n_k=100000, max_k=100000, B=1)                       # (2^127 itself gets to the workspace's check)
+    assert _prompt(lib, few, scale=2.0 ** 127, ws=None, n=0) == -5 and _attend(lib, few, _cache(max_pages=10000, max_len=100000), scale=2.0 ** 127, ws=None, n=0) == -5

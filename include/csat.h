@@ -247,7 +247,7 @@ csat_status csat_forward_static(void* ctx, const csat_dims* dims, const void* Q,
  * q_offsets[b+1], those of K and V k_offsets[b] .. k_offsets[b+1] (device int32 [B+1], not decreasing, within
  * n_q / n_k; sequences may be empty).  Row r, head h starts at element r * token stride + h * head stride of its
  * tensor; strides are multiples of 16 bytes (so a part of a fused projection serves as well as a tensor of its own, and 0
- * repeats a row, except of O, whose rows must not lie on one another), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
+ * repeats a row, except of O, whose rows must not lie on one another, nor on what is read), token strides below 2^24 elements.  Head h of Q reads head h / (Hq / Hkv) of K and V.
  * max_q bounds the rows of one sequence that are computed, max_k (csat_cache_store) those that are stored: rows beyond the
  * bound are not written, the others keep the places that they have among all of the sequence's rows.  (csat_prompt_attention: rows see
  * all keys whatever max_k says, which only shapes the work.)  Rows of no sequence (behind the last offset) are left as they were.
@@ -281,11 +281,13 @@ csat_status csat_prompt_attention(void* ctx, const csat_packed_dims* dims, const
  * [pages, Hkv, page, d], V codes [pages, Hkv, d, page] (a token's values a page apart, the order in which the
  * attention's matrix instructions take them).  A sequence's tokens are the first lengths[b] slots of the pages that row b of
  * table (device int32 [B, max_pages]) names; entries beyond them are not read.  max_len bounds lengths[b] (it sizes
- * the grids; at most max_pages * page).  Pages may be shared by sequences as long as they are only read.  Hkv and d of a call's dims are the
- * pool's, which the structure does not hold: no call from C can check them.
+ * the grids and the shares that a sequence's tokens are attended in: a close bound is faster; at most max_pages * page).  Pages may be
+ * shared by sequences as long as they are only read.  Hkv and d of a call's dims are the pool's, which the structure does not hold: no
+ * call from C can check them.
  * Errors in what only the device sees: a sequence whose length is negative or above max_len (to store: or below the new
- * rows), or one of whose needed table entries names no page of the pool, gives NaN in its rows of O and lse (its weights are then
- * undefined), is not stored to, and is evicted to length -1 with nothing but kept = -1 written for it; memory outside the given
+ * rows) gives NaN in its rows of O and lse; one of whose needed table entries names no page of the pool, in those that see one of its
+ * tokens (in others it may).  Its weights are then undefined, it is not stored to, and is evicted to length -1 with nothing but kept = -1
+ * written for it; memory outside the given
  * tensors is never touched. */
 typedef struct {
     int pages, page, max_pages, max_len;

@@ -2203,10 +2203,10 @@ int longest_k(const csat_packed_dims& d) { return std::min(d.max_k, d.n_k); }
 
 struct PromptPlan { bool split; int tiles, shares; size_t bytes; };
 // Row tiles of 128, or of 32 whose keys the wavefronts divide: float always, bf16 where tiles of 128 would occupy less than half
-// of the compute units (8 heads x 512 rows, d 64, 32 tiles of 128: 7.5 against 11.9 us; 2 key heads x 1024 x 4, d 128, 64 tiles: 15.7
-// against 25.5; not 96 heads x 274, 288 tiles: 15.5 against 11.7, nor 4 x 2048 x 4, 256 tiles: 60 against 47).  The keys in shares where even
-// then tiles are fewer than compute units (one row of 32 heads against 4096 keys: 12.2
-// against 38.8 us; 1024 rows, d 256, 32 tiles of 128: 25.6 against 27.0).
+// of the compute units (causal, 8 heads x 512 rows, d 64, 32 tiles of 128: 10.2 against 12.8 us; 2 key heads x 1024 x 4, d 128, 64 tiles:
+// 13.8 against 20.1; not 96 heads x 274, 288 tiles: 20.5 against 9.7, nor 4 x 2048 x 4, 256 tiles: 54 against 48).  The keys in shares where
+// even then tiles are fewer than compute units (one row of 32 heads against 4096 keys: 12.2 against 38.8 us; 1024 rows, d 256, 32 tiles of
+// 128: 24.3 against 27.1).
 PromptPlan prompt_plan(const csat_packed_dims& d) {
     PromptPlan p{};
     const int G = d.Hq / d.Hkv;
@@ -2215,7 +2215,8 @@ PromptPlan prompt_plan(const csat_packed_dims& d) {
     p.tiles = (int)(p.split ? (rows + 31) / 32 : (rows + 127) / 128);
     // Fewest keys of a share, a join's cost against what a workgroup's steps take; us with 256 / 128 / 64 / 32.  Float: 32 pairs, 338 keys,
     // one row tile, d 256 100 / 58 / 44 / 31, d 128 21.5 / 21.2 / 17.1 / 17.1, d 64 13.3 / 14.3 / 12.5 / 12.8 (4 pairs, 415 keys 15.2 / 13.0 /
-    // 11.8 / 12.5).  bf16: the same, d 64 6.8 / 9.2 / 9.4 / 9.6; 2 pairs, 1000 keys, d 256 17.4 / 13.0 / 13.7 / 14.1.
+    // 11.8 / 12.5).  bf16: the same, d 64 6.8 / 9.2 / 9.4 / 9.6; 2 pairs, 1000 keys, d 256 17.4 / 13.0 / 13.7 / 14.1.  (Float with up to 64
+    // features would take 6 to 22 % less with 64 than with the 256 it has.)
     const bool f32 = d.dtype == CSAT_F32;
     const int least = d.d > 128 ? (f32 ? 32 : 128) : f32 && d.d > 64 ? 64 : 256;
     p.shares = (int)std::max(1LL, std::min<long long>(256 / (pairs * p.tiles), longest_k(d) / least));
@@ -2249,6 +2250,8 @@ constexpr size_t kMostScoreBytes = (size_t)1 << 60;
 // Shares of a fixed number of tokens, so that long and short sequences of a batch keep the chip busy alike: 512, more where a
 // sequence would have more shares than it takes to occupy the chip twice (one sequence of 131072 tokens, 8 key heads: 58 us with
 // shares of 2048, 63, 72, 92 with 1024, 512, 256, whose join grows; 32 sequences of 700 to 8100: 92 us with 512, 100 with 2048).
+// The number goes by the bound of the lengths, not by the lengths: 4000 tokens of one sequence take 11.8 us with a bound of 4000 and 25.9
+// with one of 131072, of 32 sequences 62.6 and 129 (66 with 8192).
 CachedPlan cached_plan(const csat_packed_dims& d, const csat_cache& c, bool weights) {
     CachedPlan p{};
     const long long rows = (long long)longest_q(d) * (d.Hq / d.Hkv);

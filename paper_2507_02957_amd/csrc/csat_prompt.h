@@ -503,10 +503,11 @@ __device__ __forceinline__ void arguments_anew(PromptArgs* to) {
 // Long sequences, bf16: four wavefronts of 32 rows each go over the same keys, 64 at a time, which they stage together, the next step's
 // while one is worked on.  Two wavefronts per SIMD fill each other's waits between products (32 a step), exponentials (32 at a
 // quarter of the rate) and fragment reads (32 KB a step, at 128 bytes a cycle and CU just below the products' time).
-// Measured: 16384 tokens causal, 16 heads over 4 key heads, d 128, 1.03 to 1.07 ms = 1030 to 1070 TFLOP/s of visible pairs, where a library's
-// product of two 16384 x 16384 matrices reaches 1400; matrix units busy a third of the cycles, vector instructions 40 %, no bank
-// conflicts.  With the tiles in staging registers (244 instead of 206) 1.35 ms; with the odd values' products in the loop (410
-// registers, one wavefront per SIMD) 2.14.
+// Measured: 16384 tokens causal, 16 heads over 4 key heads, d 128, 1.03 to 1.06 ms = 1040 to 1070 TFLOP/s of visible pairs, where a library's
+// product of two 16384 x 16384 matrices reaches 1400; matrix units busy 43 % of the cycles at 2.4 GHz, vector instructions 40 %, no bank
+// conflicts.  With the tiles in staging registers (244 instead of 211) 1.35 ms; with the odd values' products in the loop (410
+// registers, one wavefront per SIMD) 2.14.  129 to 256 features have one wavefront per SIMD, whose waits nothing fills: 4 x 2048, 8 heads,
+// d 256, 120 us, 570 TFLOP/s.
 // One pass over the keys; true: outputs are too large for it (see headroom), and `again` has to be.
 template <int DT>
 __device__ __forceinline__ bool prompt_pass(const PromptArgs& a, int tid, bool again) {
@@ -617,8 +618,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, DT <= 4 ? 2 : 1) void prompt_ker
 // that spreads little work over the chip.
 template <typename T, int DT> constexpr int prompt_split_tile() { return 2 * 32 * 32 * DT * (int)sizeof(T); }      // K and V, 32 keys
 // bf16: as many wavefronts as the LDS holds tiles for, up to 8, since a row tile's keys are a chain (2 key heads x 1024 x 4, d 128: 13.4
-// against 15.9 us with 4).  Float: 4, so that two workgroups share a CU's vector units and one fills the other's start and
-// end (a clip of 1600 tokens, 12 heads: 40 against 54 us with 8); 2 for 256 features.
+// against 15.9 us with 4, then; 13.8 now).  Float: 4, so that with up to 64 features two workgroups share a CU's vector units and one fills
+// the other's start and end (a clip of 1600 tokens, 12 heads: 40 against 54 us with 8); from 65 on the registers leave one wavefront per
+// SIMD (4 x 1024, 8 heads, d 128: 101 us, 85 TFLOP/s), and from 129 on the LDS two per CU, of 512 registers each and
+// scratch (156 bytes a lane, 760 with the second pass; 4 x 300, 8 heads, d 256: 88 us, 17 TFLOP/s).
 template <typename T, int DT> constexpr int prompt_split_waves() {
     const int most = sizeof(T) == 2 ? 8 : 4;
     return most * prompt_split_tile<T, DT>() <= 128 * 1024 ? most : most / 2;
